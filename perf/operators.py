@@ -108,7 +108,7 @@ def draw(rng):
     cached = _log(rng, 1, 7000) if step or rng.random() < 0.4 else 0
     window, sinks = rng.choice([0, _log(rng, 1, 4096), _log(rng, 16, 4096)]), rng.choice([0, 1, 4, 4, 130])
     # score entries of the plain form, and rows held
-    entries = 1 << 30 if small else 1 << 31
+    entries = 1 << 29 if small else 9 << 27
     while q_heads * new * (new + cached) > entries:
         new, cached = (new + 1) // 2, cached // 2
     length = new + cached
