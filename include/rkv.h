@@ -308,6 +308,53 @@ RKV_API size_t rkv_decode_workspace_bytes(const rkv_desc_t *desc, int32_t budget
 RKV_API int rkv_decode_attention(const rkv_desc_t *desc, const void *k_cache, const void *v_cache, const void *q_new,
                                  const int32_t *seq_lens, float *out, int32_t budget, int32_t buffer, void *stream);
 
+/* ---- New tokens, several at a time ----------------------------------------------------------------------------------
+ * The calls below take the new tokens of a step, of a prompt or of a piece of one, packed sequence after sequence, and caches of any capacity
+ * budget + buffer up to RKV_MAX_ROWS (budget >= 1, buffer >= 0; the compression itself takes RKV_MAX_CAP).  They follow
+ * desc->block_table as the other calls do, with budget + buffer a multiple of 128 then.
+ */
+#define RKV_MAX_ROWS (1 << 20)
+
+/* The new tokens of a call.  Plain data; `offsets` is read on the device when the call runs. */
+typedef struct rkv_tokens {
+    int32_t total;          /* rows of the token tensors */
+    int32_t longest;        /* no sequence has more new tokens than this; it sizes the launch */
+    const int32_t *offsets; /* device int32 [batch + 1], 4-byte aligned, ascending from 0 up: the new tokens of sequence b are rows offsets[b] ..
+                               offsets[b + 1] - 1 (none, where the two are equal).  Rows from offsets[batch] on belong to no sequence: nothing is
+                               written there.  NULL: `longest` tokens each, total = batch * longest.  A sequence whose entries descend, leave
+                               0 .. total or hold more than `longest` tokens has no tokens in the call, and RKV_ERR_INVALID_ARG is recorded; where
+                               entries descend, which of the other sequences' tokens take part is unspecified */
+    int64_t q_stride, k_stride, v_stride, out_stride; /* elements from a token's row to the next in q, k_new, v_new and the output (a token's heads lie
+                               back to back): at least heads * head_dim, a whole number of 16-byte vectors; 0: back to back.  Slices of a fused
+                               projection are token tensors as they lie */
+} rkv_tokens_t;
+
+/* The rotation of a call: pairs of elements (x, y) of a head become (x cos - y sin, x sin + y cos). */
+typedef struct rkv_rotary {
+    const float *table;       /* device float32 [rows][dim], 16-byte aligned: the cosines of a position's dim / 2 angles, then their sines */
+    int32_t rows;             /* positions 0 .. rows - 1 */
+    int32_t dim;              /* the first dim elements of a head are rotated: a multiple of 16, at most head_dim; 0: none are (table unused) */
+    int32_t interleaved;      /* 0: element i pairs with dim / 2 + i; 1: element 2i with 2i + 1 */
+    const int32_t *positions; /* device int32 [batch]: position of the sequence's first new token, the others follow one by one.  (After a
+                                 compression a cache holds fewer rows than the sequence had tokens.)  NULL: the cache row that it enters */
+} rkv_rotary_t;
+
+/*
+ * rkv_append for several tokens per sequence, with the position rotation on the way: the new tokens' keys are rotated and enter rows seq_lens[b]
+ * .. of every KV head of sequence b, their values beside them; the queries, where given, are rotated into q_out; seq_lens[b] grows by the number of
+ * new tokens.
+ *   k_new, v_new  [total][n_kv_heads][head_dim] (device; dtype of the cache; bf16 for 8-bit caches, rounded to the nearest code, beyond the
+ *                 largest one (448) to that one)
+ *   q_new, q_out  [total][n_q_heads][head_dim] of the queries' type, both or neither NULL; q_out may be q_new (with out_stride = q_stride)
+ * Products in fp32, rounded once; what is not rotated and keeps its type is copied bit for bit.  All tensors 16-byte aligned.
+ * A sequence that the tokens do not fit into (or whose length is invalid), or whose positions leave the table, is left as it is, its rows of q_out
+ * too, and RKV_ERR_INVALID_ARG is written to desc->device_status.
+ * One launch for one token per sequence (offsets NULL, longest 1), else two; no workspace.
+ */
+RKV_API int rkv_append_rotary(const rkv_desc_t *desc, void *k_cache, void *v_cache, const void *k_new, const void *v_new,
+                              int32_t *seq_lens, int32_t budget, int32_t buffer, const rkv_tokens_t *tokens,
+                              const rkv_rotary_t *rotary, const void *q_new, void *q_out, void *stream);
+
 /*
  * Self-test of the kernels' failure detection (no counterpart in the paper).  Every wait inside the tensor-core
  * kernels is bounded; this call makes such a wait run out on purpose, in a tiny kernel of its own (one block that

@@ -9,4 +9,5 @@ from .binding import (  # noqa: F401
     rkv_compress, rkv_compress_ex, rkv_compress_stages, rkv_compress_host, rkv_compress_static,
     RKV_STATIC_SCRATCH_BYTES, rkv_desc_default, rkv_append, rkv_push_query, rkv_selftest_wait_expiry, rkv_decode_attention, rkv_decode_workspace_bytes,
     rkv_host_workspace_bytes, rkv_launch_count, rkv_launch_count_for, rkv_set_desc, rkv_status_string, rkv_workspace_bytes,
+    RkvTokens, RkvRotary, rkv_tokens, rkv_rotary, rkv_append_rotary,
 )

@@ -52,6 +52,19 @@ class RkvDesc(ctypes.Structure):
     ]
 
 
+class RkvTokens(ctypes.Structure):
+    """Mirror of rkv_tokens_t; rkv_tokens() fills one."""
+    _fields_ = [("total", ctypes.c_int32), ("longest", ctypes.c_int32), ("offsets", ctypes.c_void_p),
+                ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
+                ("out_stride", ctypes.c_int64)]
+
+
+class RkvRotary(ctypes.Structure):
+    """Mirror of rkv_rotary_t; rkv_rotary() fills one."""
+    _fields_ = [("table", ctypes.c_void_p), ("rows", ctypes.c_int32), ("dim", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("positions", ctypes.c_void_p)]
+
+
 def lib_path() -> str:
     return _LIB_PATH
 
@@ -78,6 +91,9 @@ def lib():
         L.rkv_compress_static.restype, L.rkv_compress_static.argtypes = ctypes.c_int, [P] + ten
         L.rkv_append.restype, L.rkv_append.argtypes = ctypes.c_int, [P, VP, VP, VP, VP, VP, I32, I32, VP]
         L.rkv_push_query.restype, L.rkv_push_query.argtypes = ctypes.c_int, [P, VP, VP, I32, I32, VP]
+        T, R = ctypes.POINTER(RkvTokens), ctypes.POINTER(RkvRotary)
+        L.rkv_append_rotary.restype = ctypes.c_int
+        L.rkv_append_rotary.argtypes = [P, VP, VP, VP, VP, VP, I32, I32, T, R, VP, VP, VP]
         L.rkv_decode_workspace_bytes.restype, L.rkv_decode_workspace_bytes.argtypes = SZ, [P, I32, I32]
         L.rkv_decode_attention.restype, L.rkv_decode_attention.argtypes = ctypes.c_int, [P, VP, VP, VP, VP, VP, I32, I32, VP]
         L.rkv_selftest_wait_expiry.restype, L.rkv_selftest_wait_expiry.argtypes = ctypes.c_int, [VP, VP, ctypes.c_int64, VP]
@@ -102,9 +118,9 @@ def _load_fast(L) -> None:
     if raw is None or device is None:               # (a torch built without CUDA)
         raw, device = (lambda _: _stream(None)), (lambda: 0)
     address = [ctypes.cast(f, ctypes.c_void_p).value for f in (L.rkv_push_query, L.rkv_append, L.rkv_decode_attention,
-                                                               L.rkv_compress_stages)]
-    module.bind(*address, torch.cuda.is_initialized, device, raw, lambda: _stream(None), RkvDesc,
-                ctypes.sizeof(RkvDesc))
+                                                               L.rkv_compress_stages, L.rkv_append_rotary)]
+    structs = [(t, ctypes.sizeof(t)) for t in (RkvDesc, RkvTokens, RkvRotary)]
+    module.bind(tuple(address), torch.cuda.is_initialized, device, raw, lambda: _stream(None), tuple(structs))
     _fast = module
 
 
@@ -204,6 +220,52 @@ def rkv_push_query(desc, q_window, q_new, alpha, slot, stream=None) -> int:
     if _fast is None:
         lib()
     return _fast.push_query(desc, q_window, q_new, alpha, slot, stream)
+
+
+def rkv_tokens(total: int, longest: int, offsets: Optional[torch.Tensor] = None, q_stride: int = 0, k_stride: int = 0,
+               v_stride: int = 0, out_stride: int = 0) -> RkvTokens:
+    """The packed new tokens of a call (rkv_tokens_t).  The structure keeps `offsets` (device int32 [batch + 1]) alive."""
+    if offsets is not None:
+        assert offsets.dtype == torch.int32 and offsets.is_contiguous(), "offsets must be contiguous int32"
+    t = RkvTokens(total, longest, _ptr(offsets), q_stride, k_stride, v_stride, out_stride)
+    t.kept = offsets
+    return t
+
+
+def rkv_rotary(table: Optional[torch.Tensor], dim: int, positions: Optional[torch.Tensor] = None,
+               interleaved: bool = False) -> RkvRotary:
+    """The rotation of a call (rkv_rotary_t): table float32 [rows, dim], the cosines and then the sines of a position's angles;
+    positions int32 [batch].  The structure keeps both alive."""
+    if dim and table is not None:
+        assert table.dtype == torch.float32 and table.dim() == 2 and table.shape[1] == dim, "table must be float32 [rows, dim]"
+    if positions is not None:
+        assert positions.dtype == torch.int32, "positions must be int32"
+    r = RkvRotary(_ptr(table), 0 if table is None else table.shape[0], dim, int(interleaved), _ptr(positions))
+    r.kept = (table, positions)
+    return r
+
+
+def _token_rows(t, stride: int):
+    """The data pointer of a token tensor [total, heads, head_dim] whose rows are `stride` elements apart (0: contiguous)."""
+    if t is None or isinstance(t, int) or stride == 0:
+        return t                     # (a tensor's contiguity is checked where its pointer is taken)
+    row = 1
+    for size, step in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
+        assert size == 1 or step == row, "a token's heads must lie back to back"
+        row *= size
+    assert t.shape[0] <= 1 or t.stride(0) == stride, "the tensor's rows are not the tokens' stride apart"
+    return t.data_ptr()
+
+
+def rkv_append_rotary(desc, k_cache, v_cache, k_new, v_new, seq_lens, budget, buffer, tokens, rotary, q_new=None, q_out=None,
+                      stream=None) -> int:
+    """The new tokens' keys, rotated by their positions, and their values enter the caches from row seq_lens[b] on; their
+    queries, where given, are rotated into q_out; seq_lens[b] grows by the sequence's new tokens."""
+    if _fast is None:
+        lib()
+    return _fast.append_rotary(desc, k_cache, v_cache, _token_rows(k_new, tokens.k_stride), _token_rows(v_new, tokens.v_stride),
+                               seq_lens, budget, buffer, tokens, rotary, _token_rows(q_new, tokens.q_stride),
+                               _token_rows(q_out, tokens.out_stride), stream)
 
 
 def rkv_decode_workspace_bytes(desc, budget: int, buffer: int) -> int:

@@ -13,17 +13,21 @@ typedef int (*append_fn)(const void *, void *, void *, const void *, const void 
 typedef int (*attend_fn)(const void *, const void *, const void *, const void *, const int32_t *, float *, int32_t, int32_t, void *);
 typedef int (*stages_fn)(const void *, void *, void *, const void *, int32_t *, int32_t, int32_t, int32_t, float, int32_t *, void *,
                          uint32_t);
+typedef int (*append_rotary_fn)(const void *, void *, void *, const void *, const void *, int32_t *, int32_t, int32_t, const void *,
+                                const void *, const void *, void *, void *);
 
 static push_fn g_push;
 static append_fn g_append;
 static attend_fn g_attend;
 static stages_fn g_stages;
+static append_rotary_fn g_append_rotary;
 static PyObject *g_device, *g_raw_stream;    /* current device; its current stream's handle */
 static PyObject *g_slow_stream;              /* the binding's own answer, asked until CUDA is initialised */
 static PyObject *g_initialised;
 static int g_ready;
-static PyObject *g_desc_type;                /* the binding's descriptor structure, and its size */
-static Py_ssize_t g_desc_size;
+enum { kDesc, kTokens, kRotary, kStructs };
+static PyObject *g_type[kStructs];           /* the binding's structures, and their sizes */
+static Py_ssize_t g_size[kStructs];
 static PyObject *s_contiguous, *s_data_ptr, *s_cuda_stream;
 
 static int get_ptr(PyObject *o, void **out)
@@ -98,21 +102,22 @@ static int get_int(PyObject *o, int32_t *out)
     return PyErr_Occurred() ? -1 : 0;
 }
 
-/* the descriptor (a ctypes structure of the binding's type, nothing else that has bytes) stays where it is while `view` is held */
-static int get_desc(PyObject *o, Py_buffer *view)
+/* a ctypes structure of the binding's type `which`, nothing else that has bytes; it stays where it is while `view` is held */
+static int get_struct(PyObject *o, int which, Py_buffer *view)
 {
-    const int is = (PyObject *)Py_TYPE(o) == g_desc_type ? 1 : PyObject_IsInstance(o, g_desc_type);
+    const int is = (PyObject *)Py_TYPE(o) == g_type[which] ? 1 : PyObject_IsInstance(o, g_type[which]);
     if (is < 0) return -1;
     if (!is) {
-        PyErr_Format(PyExc_TypeError, "expected an RkvDesc, got %s", Py_TYPE(o)->tp_name);
+        PyErr_Format(PyExc_TypeError, "expected an %s, got %s", ((PyTypeObject *)g_type[which])->tp_name, Py_TYPE(o)->tp_name);
         return -1;
     }
     if (PyObject_GetBuffer(o, view, PyBUF_SIMPLE)) return -1;
-    if (view->len >= g_desc_size) return 0;
+    if (view->len >= g_size[which]) return 0;
     PyBuffer_Release(view);
-    PyErr_SetString(PyExc_TypeError, "the descriptor is too small");
+    PyErr_Format(PyExc_TypeError, "the %s is too small", which == kDesc ? "descriptor" : "structure");
     return -1;
 }
+static int get_desc(PyObject *o, Py_buffer *view) { return get_struct(o, kDesc, view); }
 
 static int want(Py_ssize_t n, Py_ssize_t expected)
 {
@@ -187,22 +192,56 @@ static PyObject *compress_stages(PyObject *self, PyObject *const *a, Py_ssize_t 
     return PyLong_FromLong(rc);
 }
 
-/* (addresses of rkv_push_query, rkv_append, rkv_decode_attention, rkv_compress_stages; is_initialised, current_device,
- *  raw_stream(device), slow_stream; the descriptor's type and size) */
+/* (desc, k_cache, v_cache, k_new, v_new, seq_lens, budget, buffer, tokens, rotary, q_new, q_out, stream) */
+static PyObject *append_rotary(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    void *t[5], *q[2], *s;
+    int32_t budget, buffer;
+    Py_buffer d, tok, rot;
+    int rc;
+    if (want(n, 13)) return NULL;
+    for (int i = 0; i < 5; ++i)
+        if (get_ptr(a[1 + i], &t[i])) return NULL;
+    if (get_int(a[6], &budget) || get_int(a[7], &buffer) || get_ptr(a[10], &q[0]) || get_ptr(a[11], &q[1]) || get_stream(a[12], &s) ||
+        get_desc(a[0], &d))
+        return NULL;
+    if (get_struct(a[8], kTokens, &tok)) goto no_tokens;
+    if (get_struct(a[9], kRotary, &rot)) goto no_rotary;
+    Py_BEGIN_ALLOW_THREADS rc = g_append_rotary(d.buf, t[0], t[1], t[2], t[3], t[4], budget, buffer, tok.buf, rot.buf, q[0], q[1], s);
+    Py_END_ALLOW_THREADS PyBuffer_Release(&rot);
+    PyBuffer_Release(&tok);
+    PyBuffer_Release(&d);
+    return PyLong_FromLong(rc);
+no_rotary:
+    PyBuffer_Release(&tok);
+no_tokens:
+    PyBuffer_Release(&d);
+    return NULL;
+}
+
+/* ((addresses of rkv_push_query, rkv_append, rkv_decode_attention, rkv_compress_stages, rkv_append_rotary), is_initialised,
+ *  current_device, raw_stream(device), slow_stream, ((structure, size) of the descriptor, the tokens and the rotation)) */
 static PyObject *bind(PyObject *self, PyObject *args)
 {
-    unsigned long long f[4];
-    PyObject *o[5];
-    if (!PyArg_ParseTuple(args, "KKKKOOOOOn", &f[0], &f[1], &f[2], &f[3], &o[0], &o[1], &o[2], &o[3], &o[4], &g_desc_size)) return NULL;
+    unsigned long long f[5];
+    PyObject *o[4], *type[kStructs];
+    Py_ssize_t size[kStructs];
+    if (!PyArg_ParseTuple(args, "(KKKKK)OOOO((On)(On)(On))", &f[0], &f[1], &f[2], &f[3], &f[4], &o[0], &o[1], &o[2], &o[3], &type[0],
+                          &size[0], &type[1], &size[1], &type[2], &size[2]))
+        return NULL;
     g_push = (push_fn)(uintptr_t)f[0];
     g_append = (append_fn)(uintptr_t)f[1];
     g_attend = (attend_fn)(uintptr_t)f[2];
     g_stages = (stages_fn)(uintptr_t)f[3];
+    g_append_rotary = (append_rotary_fn)(uintptr_t)f[4];
     Py_XSETREF(g_initialised, Py_NewRef(o[0]));
     Py_XSETREF(g_device, Py_NewRef(o[1]));
     Py_XSETREF(g_raw_stream, Py_NewRef(o[2]));
     Py_XSETREF(g_slow_stream, Py_NewRef(o[3]));
-    Py_XSETREF(g_desc_type, Py_NewRef(o[4]));
+    for (int i = 0; i < kStructs; ++i) {
+        Py_XSETREF(g_type[i], Py_NewRef(type[i]));
+        g_size[i] = size[i];
+    }
     Py_RETURN_NONE;
 }
 
@@ -210,6 +249,7 @@ static PyMethodDef g_methods[] = {{"push_query", (PyCFunction)(void (*)(void))pu
                                   {"append", (PyCFunction)(void (*)(void))append, METH_FASTCALL, NULL},
                                   {"decode_attention", (PyCFunction)(void (*)(void))decode_attention, METH_FASTCALL, NULL},
                                   {"compress_stages", (PyCFunction)(void (*)(void))compress_stages, METH_FASTCALL, NULL},
+                                  {"append_rotary", (PyCFunction)(void (*)(void))append_rotary, METH_FASTCALL, NULL},
                                   {"bind", bind, METH_VARARGS, NULL},
                                   {NULL, NULL, 0, NULL}};
 

@@ -17,11 +17,15 @@ thread_local rkv_desc_t g_desc;
 thread_local bool g_desc_set = false;
 thread_local char g_cuda_error[256] = "";
 
+}  // namespace
+
 int cuda_fail(cudaError_t e, const char *where)
 {
     snprintf(g_cuda_error, sizeof(g_cuda_error), "%s: %s", where, cudaGetErrorString(e));
     return RKV_ERR_CUDA;
 }
+
+namespace {
 
 struct Layout {
     size_t k_wide, q_wide, best, dense, dense_items, inv_norm, norm_split, thr_split, tile_sum, logits, row_stat, keys, sbar, left, lacking, strag, strag_items, self_dot, head_sum_bf16, meta, counters, total;
@@ -115,8 +119,6 @@ int check_shapes(const rkv_desc_t *d, int budget, int buffer, int alpha, Layout 
     }
     return RKV_OK;
 }
-
-bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // What a compression asks of its descriptor and lambda beside the shapes and the tensors.
 int check_settings(const rkv_desc_t *d, float lambda)

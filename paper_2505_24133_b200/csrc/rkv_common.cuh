@@ -294,6 +294,9 @@ inline cudaError_t allow_smem_once(PerDevice &done, int dev, Kernel kernel, int 
     return e;
 }
 
+inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+int cuda_fail(cudaError_t e, const char *where);      // keeps the error's text for rkv_last_cuda_error(); RKV_ERR_CUDA
+
 size_t compression_bytes(const rkv_desc_t *d, int budget, int buffer, int alpha);     // scratch of a compression alone; 0: invalid
 
 // launchers (one per stage); each returns cudaGetLastError() of its launch

@@ -1,0 +1,86 @@
+"""Argument checks of the calls on several new tokens per sequence: no CUDA call is made on these paths, and the fake pointers are never read."""
+import ctypes
+
+import pytest
+import torch
+
+
+@pytest.fixture(scope="module")
+def rkv():
+    from paper_2505_24133_b200 import build as b
+    b.build()
+    import paper_2505_24133_b200 as r
+    return r
+
+
+def _desc(rkv, **kw):
+    d = rkv.rkv_desc_default()
+    d.batch, d.n_kv_heads, d.n_q_heads = 2, 8, 32
+    for k, v in kw.items():
+        setattr(d, k, v)
+    return d
+
+
+def _tokens(rkv, **kw):
+    t = rkv.rkv_tokens(20, 16)
+    t.offsets = 0x30000
+    for k, v in kw.items():
+        setattr(t, k, v)
+    return t
+
+
+GOOD = 0x20000
+
+
+@pytest.mark.parametrize("case,want", [
+    (dict(k_cache=None), 1), (dict(v_new=None), 1), (dict(seq=None), 1), (dict(k_new=GOOD + 8), 1), (dict(q_out=GOOD + 2), 1),
+    (dict(q_out=None), 1), (dict(q_new=None), 1), (dict(seq=GOOD + 2), 1), (dict(budget=0), 1), (dict(buffer=-1), 1),
+    (dict(budget=1 << 20, buffer=1), 2), (dict(desc=dict(head_dim=96)), 2), (dict(desc=dict(dtype=7)), 2), (dict(desc=dict(n_q_heads=30)), 1),
+    (dict(desc=dict(batch=0)), 1), (dict(desc=dict(block_table=GOOD, pool_pages=0), budget=128, buffer=0), 1),
+    (dict(desc=dict(block_table=GOOD, pool_pages=9), budget=100, buffer=1), 1), (dict(desc=dict(block_table=GOOD + 1, pool_pages=9), budget=128, buffer=0), 1),
+    (dict(tokens=dict(total=-1)), 1), (dict(tokens=dict(longest=0)), 1), (dict(tokens=dict(offsets=0x30001)), 1),
+    (dict(tokens=dict(offsets=None)), 1), (dict(tokens=dict(total=1 << 27)), 2),
+    (dict(tokens=dict(k_stride=1023)), 1), (dict(tokens=dict(k_stride=1028)), 1), (dict(tokens=dict(q_stride=4095)), 1),
+    (dict(tokens=dict(out_stride=-4096)), 1), (dict(tokens=dict(v_stride=1 << 62)), 1),
+    (dict(rotary=dict(dim=8)), 1), (dict(rotary=dict(dim=144)), 1), (dict(rotary=dict(dim=-16)), 1), (dict(rotary=dict(table=None)), 1),
+    (dict(rotary=dict(table=GOOD + 4)), 1), (dict(rotary=dict(rows=0)), 1), (dict(rotary=dict(positions=GOOD + 1)), 1),
+    (dict(q_new=GOOD, q_out=GOOD, tokens=dict(q_stride=8192)), 1),
+    (dict(tokens=dict(total=0)), 0), (dict(tokens=dict(total=0), q_new=None, q_out=None), 0),
+])
+def test_append_rotary_refuses(rkv, case, want):
+    a = dict(k_cache=GOOD, v_cache=GOOD, k_new=GOOD, v_new=GOOD, seq=GOOD, q_new=GOOD, q_out=2 * GOOD, budget=1024, buffer=128)
+    a.update({k: v for k, v in case.items() if k in a})
+    rotary = rkv.rkv_rotary(None, 128)
+    rotary.table, rotary.rows = GOOD, 100
+    for k, v in case.get("rotary", {}).items():
+        setattr(rotary, k, v)
+    got = rkv.rkv_append_rotary(_desc(rkv, **case.get("desc", {})), a["k_cache"], a["v_cache"], a["k_new"], a["v_new"], a["seq"], a["budget"],
+                                a["buffer"], _tokens(rkv, **case.get("tokens", {})), rotary, a["q_new"], a["q_out"], 0)
+    assert got == want
+
+
+def test_structures_are_taken_as_what_they_are(rkv):
+    d, t, r = _desc(rkv), _tokens(rkv), rkv.rkv_rotary(None, 0)
+    call = lambda d, t, r: rkv.rkv_append_rotary(d, None, None, None, None, None, 64, 32, t, r, None, None, 0)  # noqa: E731
+    assert call(d, t, r) == 1                                     # null tensors
+    for bad in ((t, t, r), (d, t, t), (d, t, d)):
+        with pytest.raises(TypeError):
+            call(*bad)
+    for bad in (b"0" * 64, None, (ctypes.c_char * 64)()):
+        with pytest.raises(TypeError):
+            call(bad, t, r)
+        with pytest.raises(TypeError):
+            call(d, t, bad)
+
+
+def test_token_tensors_have_the_strides_they_are_said_to_have(rkv):
+    d, r = _desc(rkv, n_kv_heads=2, n_q_heads=2, head_dim=64), rkv.rkv_rotary(None, 0)
+    qkv = torch.zeros(4, 6, 64, dtype=torch.bfloat16)
+    t = rkv.rkv_tokens(4, 4, k_stride=384, v_stride=384)
+    with pytest.raises(AssertionError):
+        rkv.rkv_append_rotary(d, None, None, qkv[:, :2].contiguous(), qkv[:, 2:4], None, 64, 32, t, r, None, None, 0)
+    with pytest.raises(AssertionError):
+        rkv.rkv_append_rotary(d, None, None, qkv[:, 0:4:2], qkv[:, 2:4], None, 64, 32, t, r, None, None, 0)
+    with pytest.raises(AssertionError):                           # strided, but the call was not told
+        rkv.rkv_append_rotary(d, None, None, qkv[:, :2], qkv[:, 2:4], None, 64, 32, rkv.rkv_tokens(4, 4), r, None, None, 0)
+    assert rkv.rkv_append_rotary(d, None, None, qkv[:, :2], qkv[:, 2:4], None, 64, 32, t, r, None, None, 0) == 1
