@@ -356,6 +356,54 @@ RKV_API int rkv_append_rotary(const rkv_desc_t *desc, void *k_cache, void *v_cac
                               const rkv_rotary_t *rotary, const void *q_new, void *q_out, void *stream);
 
 /*
+ * Attention of new tokens over caches that hold them already (rkv_append_rotary before it): prompts, pieces of prompts, single tokens.  With n =
+ * the sequence's new tokens, token t (0 .. n - 1) stands in row r = seq_lens[b] - n + t and sees the rows
+ *   j <= r  with  r - j < window  or  j < sinks        (window 0: all j <= r)
+ *   out[t][q] = sum_j softmax_j( q[t][q] . K[b][q / G][j] / sqrt(head_dim) ) V[b][q / G][j]
+ *   q    [total][n_q_heads][head_dim] (device; desc->dtype, bf16 for 8-bit caches)
+ *   out  the same shape and type as q (device); out_stride of `tokens` is its rows' distance
+ *   window >= 0, sinks >= 0
+ * Rows of the caches that no new token sees are not read, nor their pages' entries where a whole page of 128 rows is such, and may hold
+ * anything; the rows that some new token sees hold finite values (a NaN or infinity there may reach every new token of the sequence).  A sequence
+ * whose length is invalid or less than its new tokens gives zero rows and RKV_ERR_INVALID_ARG in desc->device_status; so does a page that does not
+ * exist, whose rows count as zeros.
+ * bf16 and 8-bit caches: bf16 products on the tensor cores, fp32 accumulation and softmax; fp32 caches: fp32 throughout.
+ * head_dim 64, 128 or 256, any group.  desc->workspace holds rkv_window_workspace_bytes() (0 for calls that fill the GPU): partial results of calls
+ * whose keys are split between blocks.  Enqueues one or two kernels on `stream`.
+ */
+RKV_API size_t rkv_window_workspace_bytes(const rkv_desc_t *desc, int32_t budget, int32_t buffer, const rkv_tokens_t *tokens,
+                                          int32_t window, int32_t sinks);
+RKV_API int rkv_window_attention(const rkv_desc_t *desc, const void *k_cache, const void *v_cache, const void *q,
+                                 const int32_t *seq_lens, void *out, int32_t budget, int32_t buffer, const rkv_tokens_t *tokens,
+                                 int32_t window, int32_t sinks, void *stream);
+
+/* The prompts that the sequences of a batch were sampled from (the paper draws many responses per question), each stored once. */
+typedef struct rkv_prefix {
+    const void *k, *v;    /* device, dtype of the caches, 16-byte aligned: [count][n_kv_heads][rows][head_dim], or page pools (below) */
+    int32_t count;        /* sequence b has prefix b / (batch / count); batch is a multiple of count */
+    int32_t rows;         /* capacity, 1 .. RKV_MAX_ROWS */
+    const int32_t *lens;  /* device int32 [count]: cached rows of each prefix, 0 .. rows */
+    const int32_t *table; /* optional device int32 [count][n_kv_heads][rows / 128]: pages of the pools k, v [pages][128][head_dim], as
+                             rkv_desc_t.block_table; rows a multiple of 128 then */
+    int64_t pages;
+} rkv_prefix_t;
+
+/*
+ * rkv_decode_attention for a batch that shares long prefixes: every sequence's query attends over its prefix's rows and its own cache, in one
+ * softmax; a prefix's keys and values are read once for all of its sequences.
+ *   q_new, out  [batch][n_q_heads][head_dim] as in rkv_window_attention (out has q_new's type)
+ *   seq_lens    [batch], own rows of each sequence, 0 allowed; a value outside [0, budget + buffer], like a prefix length outside [0, rows], counts as 0
+ *               and is recorded as RKV_ERR_INVALID_ARG
+ * The sequences' own caches may be compressed, appended to and paged as ever; the prefix is not compressed with them.
+ * head_dim, groups, types and arithmetic as rkv_window_attention; rows beyond the lengths are not read.  desc->workspace holds
+ * rkv_prefix_workspace_bytes().  Enqueues up to three kernels on `stream`.
+ */
+RKV_API size_t rkv_prefix_workspace_bytes(const rkv_desc_t *desc, int32_t budget, int32_t buffer, const rkv_prefix_t *prefix);
+RKV_API int rkv_prefix_attention(const rkv_desc_t *desc, const void *k_cache, const void *v_cache, const void *q_new,
+                                 const int32_t *seq_lens, void *out, int32_t budget, int32_t buffer, const rkv_prefix_t *prefix,
+                                 void *stream);
+
+/*
  * Self-test of the kernels' failure detection (no counterpart in the paper).  Every wait inside the tensor-core
  * kernels is bounded; this call makes such a wait run out on purpose, in a tiny kernel of its own (one block that
  * allocates tensor memory, waits with the given limit on a barrier nothing arrives at, calls off a second waiting

@@ -10,4 +10,5 @@ from .binding import (  # noqa: F401
     RKV_STATIC_SCRATCH_BYTES, rkv_desc_default, rkv_append, rkv_push_query, rkv_selftest_wait_expiry, rkv_decode_attention, rkv_decode_workspace_bytes,
     rkv_host_workspace_bytes, rkv_launch_count, rkv_launch_count_for, rkv_set_desc, rkv_status_string, rkv_workspace_bytes,
     RkvTokens, RkvRotary, rkv_tokens, rkv_rotary, rkv_append_rotary,
+    rkv_window_workspace_bytes, rkv_window_attention, RkvPrefix, rkv_prefix, rkv_prefix_workspace_bytes, rkv_prefix_attention,
 )

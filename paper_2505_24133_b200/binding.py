@@ -65,6 +65,12 @@ class RkvRotary(ctypes.Structure):
                 ("interleaved", ctypes.c_int32), ("positions", ctypes.c_void_p)]
 
 
+class RkvPrefix(ctypes.Structure):
+    """Mirror of rkv_prefix_t; rkv_prefix() fills one."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("count", ctypes.c_int32), ("rows", ctypes.c_int32),
+                ("lens", ctypes.c_void_p), ("table", ctypes.c_void_p), ("pages", ctypes.c_int64)]
+
+
 def lib_path() -> str:
     return _LIB_PATH
 
@@ -94,6 +100,12 @@ def lib():
         T, R = ctypes.POINTER(RkvTokens), ctypes.POINTER(RkvRotary)
         L.rkv_append_rotary.restype = ctypes.c_int
         L.rkv_append_rotary.argtypes = [P, VP, VP, VP, VP, VP, I32, I32, T, R, VP, VP, VP]
+        X = ctypes.POINTER(RkvPrefix)
+        L.rkv_window_workspace_bytes.restype, L.rkv_window_workspace_bytes.argtypes = SZ, [P, I32, I32, T, I32, I32]
+        L.rkv_window_attention.restype = ctypes.c_int
+        L.rkv_window_attention.argtypes = [P, VP, VP, VP, VP, VP, I32, I32, T, I32, I32, VP]
+        L.rkv_prefix_workspace_bytes.restype, L.rkv_prefix_workspace_bytes.argtypes = SZ, [P, I32, I32, X]
+        L.rkv_prefix_attention.restype, L.rkv_prefix_attention.argtypes = ctypes.c_int, [P, VP, VP, VP, VP, VP, I32, I32, X, VP]
         L.rkv_decode_workspace_bytes.restype, L.rkv_decode_workspace_bytes.argtypes = SZ, [P, I32, I32]
         L.rkv_decode_attention.restype, L.rkv_decode_attention.argtypes = ctypes.c_int, [P, VP, VP, VP, VP, VP, I32, I32, VP]
         L.rkv_selftest_wait_expiry.restype, L.rkv_selftest_wait_expiry.argtypes = ctypes.c_int, [VP, VP, ctypes.c_int64, VP]
@@ -118,8 +130,9 @@ def _load_fast(L) -> None:
     if raw is None or device is None:               # (a torch built without CUDA)
         raw, device = (lambda _: _stream(None)), (lambda: 0)
     address = [ctypes.cast(f, ctypes.c_void_p).value for f in (L.rkv_push_query, L.rkv_append, L.rkv_decode_attention,
-                                                               L.rkv_compress_stages, L.rkv_append_rotary)]
-    structs = [(t, ctypes.sizeof(t)) for t in (RkvDesc, RkvTokens, RkvRotary)]
+                                                               L.rkv_compress_stages, L.rkv_append_rotary,
+                                                               L.rkv_window_attention, L.rkv_prefix_attention)]
+    structs = [(t, ctypes.sizeof(t)) for t in (RkvDesc, RkvTokens, RkvRotary, RkvPrefix)]
     module.bind(tuple(address), torch.cuda.is_initialized, device, raw, lambda: _stream(None), tuple(structs))
     _fast = module
 
@@ -266,6 +279,44 @@ def rkv_append_rotary(desc, k_cache, v_cache, k_new, v_new, seq_lens, budget, bu
     return _fast.append_rotary(desc, k_cache, v_cache, _token_rows(k_new, tokens.k_stride), _token_rows(v_new, tokens.v_stride),
                                seq_lens, budget, buffer, tokens, rotary, _token_rows(q_new, tokens.q_stride),
                                _token_rows(q_out, tokens.out_stride), stream)
+
+
+def rkv_window_workspace_bytes(desc, budget: int, buffer: int, tokens: RkvTokens, window: int, sinks: int) -> int:
+    return int(lib().rkv_window_workspace_bytes(ctypes.byref(desc), budget, buffer, ctypes.byref(tokens), window, sinks))
+
+
+def rkv_window_attention(desc, k_cache, v_cache, q, seq_lens, out, budget, buffer, tokens, window, sinks, stream=None) -> int:
+    """Attention of new tokens over the caches that hold them already: each sees the rows up to its own that lie among the last
+    `window` (0: all) or among the first `sinks`; out has q's shape and type."""
+    if _fast is None:
+        lib()
+    return _fast.window_attention(desc, k_cache, v_cache, _token_rows(q, tokens.q_stride), seq_lens, _token_rows(out, tokens.out_stride),
+                                  budget, buffer, tokens, window, sinks, stream)
+
+
+def rkv_prefix(k: torch.Tensor, v: torch.Tensor, lens: torch.Tensor, table: Optional[torch.Tensor] = None) -> RkvPrefix:
+    """Prefixes that sequences share (rkv_prefix_t): k, v [count, n_kv_heads, rows, head_dim] and lens int32 [count], or, with
+    table int32 [count, n_kv_heads, rows / 128], page pools [pages, 128, head_dim].  The structure keeps them alive."""
+    assert lens.dtype == torch.int32 and k.shape == v.shape, "lens must be int32, k and v of one shape"
+    if table is None:
+        x = RkvPrefix(_ptr(k), _ptr(v), k.shape[0], k.shape[2], _ptr(lens), None, 0)
+    else:
+        assert table.dtype == torch.int32, "table must be int32"
+        x = RkvPrefix(_ptr(k), _ptr(v), table.shape[0], table.shape[2] * 128, _ptr(lens), _ptr(table), k.shape[0])
+    x.kept = (k, v, lens, table)
+    return x
+
+
+def rkv_prefix_workspace_bytes(desc, budget: int, buffer: int, prefix: RkvPrefix) -> int:
+    return int(lib().rkv_prefix_workspace_bytes(ctypes.byref(desc), budget, buffer, ctypes.byref(prefix)))
+
+
+def rkv_prefix_attention(desc, k_cache, v_cache, q_new, seq_lens, out, budget, buffer, prefix, stream=None) -> int:
+    """One decode step of sequences that share prefixes: every query attends over its prefix and its own cache in one softmax;
+    out has q_new's shape and type."""
+    if _fast is None:
+        lib()
+    return _fast.prefix_attention(desc, k_cache, v_cache, q_new, seq_lens, out, budget, buffer, prefix, stream)
 
 
 def rkv_decode_workspace_bytes(desc, budget: int, buffer: int) -> int:

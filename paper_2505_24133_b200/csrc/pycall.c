@@ -15,17 +15,23 @@ typedef int (*stages_fn)(const void *, void *, void *, const void *, int32_t *, 
                          uint32_t);
 typedef int (*append_rotary_fn)(const void *, void *, void *, const void *, const void *, int32_t *, int32_t, int32_t, const void *,
                                 const void *, const void *, void *, void *);
+typedef int (*window_fn)(const void *, const void *, const void *, const void *, const int32_t *, void *, int32_t, int32_t, const void *,
+                         int32_t, int32_t, void *);
+typedef int (*prefix_fn)(const void *, const void *, const void *, const void *, const int32_t *, void *, int32_t, int32_t, const void *,
+                         void *);
 
 static push_fn g_push;
 static append_fn g_append;
 static attend_fn g_attend;
 static stages_fn g_stages;
 static append_rotary_fn g_append_rotary;
+static window_fn g_window;
+static prefix_fn g_prefix;
 static PyObject *g_device, *g_raw_stream;    /* current device; its current stream's handle */
 static PyObject *g_slow_stream;              /* the binding's own answer, asked until CUDA is initialised */
 static PyObject *g_initialised;
 static int g_ready;
-enum { kDesc, kTokens, kRotary, kStructs };
+enum { kDesc, kTokens, kRotary, kPrefix, kStructs };
 static PyObject *g_type[kStructs];           /* the binding's structures, and their sizes */
 static Py_ssize_t g_size[kStructs];
 static PyObject *s_contiguous, *s_data_ptr, *s_cuda_stream;
@@ -219,21 +225,68 @@ no_tokens:
     return NULL;
 }
 
-/* ((addresses of rkv_push_query, rkv_append, rkv_decode_attention, rkv_compress_stages, rkv_append_rotary), is_initialised,
- *  current_device, raw_stream(device), slow_stream, ((structure, size) of the descriptor, the tokens and the rotation)) */
+/* (desc, k_cache, v_cache, q, seq_lens, out, budget, buffer, tokens, window, sinks, stream) */
+static PyObject *window_attention(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    void *t[5], *s;
+    int32_t budget, buffer, window, sinks;
+    Py_buffer d, tok;
+    int rc;
+    if (want(n, 12)) return NULL;
+    for (int i = 0; i < 5; ++i)
+        if (get_ptr(a[1 + i], &t[i])) return NULL;
+    if (get_int(a[6], &budget) || get_int(a[7], &buffer) || get_int(a[9], &window) || get_int(a[10], &sinks) || get_stream(a[11], &s) ||
+        get_desc(a[0], &d))
+        return NULL;
+    if (get_struct(a[8], kTokens, &tok)) {
+        PyBuffer_Release(&d);
+        return NULL;
+    }
+    Py_BEGIN_ALLOW_THREADS rc = g_window(d.buf, t[0], t[1], t[2], t[3], t[4], budget, buffer, tok.buf, window, sinks, s);
+    Py_END_ALLOW_THREADS PyBuffer_Release(&tok);
+    PyBuffer_Release(&d);
+    return PyLong_FromLong(rc);
+}
+
+/* (desc, k_cache, v_cache, q_new, seq_lens, out, budget, buffer, prefix, stream) */
+static PyObject *prefix_attention(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    void *t[5], *s;
+    int32_t budget, buffer;
+    Py_buffer d, x;
+    int rc;
+    if (want(n, 10)) return NULL;
+    for (int i = 0; i < 5; ++i)
+        if (get_ptr(a[1 + i], &t[i])) return NULL;
+    if (get_int(a[6], &budget) || get_int(a[7], &buffer) || get_stream(a[9], &s) || get_desc(a[0], &d)) return NULL;
+    if (get_struct(a[8], kPrefix, &x)) {
+        PyBuffer_Release(&d);
+        return NULL;
+    }
+    Py_BEGIN_ALLOW_THREADS rc = g_prefix(d.buf, t[0], t[1], t[2], t[3], t[4], budget, buffer, x.buf, s);
+    Py_END_ALLOW_THREADS PyBuffer_Release(&x);
+    PyBuffer_Release(&d);
+    return PyLong_FromLong(rc);
+}
+
+/* ((addresses of rkv_push_query, rkv_append, rkv_decode_attention, rkv_compress_stages, rkv_append_rotary, rkv_window_attention,
+ *  rkv_prefix_attention), is_initialised, current_device, raw_stream(device), slow_stream, ((structure, size) of the descriptor, the
+ *  tokens, the rotation and the prefixes)) */
 static PyObject *bind(PyObject *self, PyObject *args)
 {
-    unsigned long long f[5];
+    unsigned long long f[7];
     PyObject *o[4], *type[kStructs];
     Py_ssize_t size[kStructs];
-    if (!PyArg_ParseTuple(args, "(KKKKK)OOOO((On)(On)(On))", &f[0], &f[1], &f[2], &f[3], &f[4], &o[0], &o[1], &o[2], &o[3], &type[0],
-                          &size[0], &type[1], &size[1], &type[2], &size[2]))
+    if (!PyArg_ParseTuple(args, "(KKKKKKK)OOOO((On)(On)(On)(On))", &f[0], &f[1], &f[2], &f[3], &f[4], &f[5], &f[6], &o[0], &o[1], &o[2],
+                          &o[3], &type[0], &size[0], &type[1], &size[1], &type[2], &size[2], &type[3], &size[3]))
         return NULL;
     g_push = (push_fn)(uintptr_t)f[0];
     g_append = (append_fn)(uintptr_t)f[1];
     g_attend = (attend_fn)(uintptr_t)f[2];
     g_stages = (stages_fn)(uintptr_t)f[3];
     g_append_rotary = (append_rotary_fn)(uintptr_t)f[4];
+    g_window = (window_fn)(uintptr_t)f[5];
+    g_prefix = (prefix_fn)(uintptr_t)f[6];
     Py_XSETREF(g_initialised, Py_NewRef(o[0]));
     Py_XSETREF(g_device, Py_NewRef(o[1]));
     Py_XSETREF(g_raw_stream, Py_NewRef(o[2]));
@@ -250,6 +303,8 @@ static PyMethodDef g_methods[] = {{"push_query", (PyCFunction)(void (*)(void))pu
                                   {"decode_attention", (PyCFunction)(void (*)(void))decode_attention, METH_FASTCALL, NULL},
                                   {"compress_stages", (PyCFunction)(void (*)(void))compress_stages, METH_FASTCALL, NULL},
                                   {"append_rotary", (PyCFunction)(void (*)(void))append_rotary, METH_FASTCALL, NULL},
+                                  {"window_attention", (PyCFunction)(void (*)(void))window_attention, METH_FASTCALL, NULL},
+                                  {"prefix_attention", (PyCFunction)(void (*)(void))prefix_attention, METH_FASTCALL, NULL},
                                   {"bind", bind, METH_VARARGS, NULL},
                                   {NULL, NULL, 0, NULL}};
 

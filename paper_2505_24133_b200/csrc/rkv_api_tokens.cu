@@ -38,6 +38,97 @@ int check_tokens(const rkv_desc_t *d, const rkv_tokens_t *t, TokenMap *m)
     return RKV_OK;
 }
 
+int sm_count()
+{
+    int dev = 0, sms = 0;
+    return device_sms(&dev, &sms) == cudaSuccess ? sms : 148;    // sizing only (no device here): the B200's count
+}
+
+// Query rows of 64 to a block: the tiles of 128 keys that such a block may come to are shared out until there are two waves of blocks (two to
+// an SM).
+constexpr int kSimtRows = 64, kMaxSplits = 64;
+int simt_splits(const RowsParams &p)
+{
+    const long long blocks = ((long long)p.tokens.longest * p.group + kSimtRows - 1) / kSimtRows * p.hkv * p.tokens.count;
+    const long long seen = p.causal && p.window > 0 ? (long long)p.window + kSimtRows / p.group + 1 : p.cap;
+    const long long tiles = (seen < p.cap ? seen / kTile + 2 + (p.sinks + kTile - 1) / kTile : (p.cap + kTile - 1) / kTile);
+    long long splits = (4ll * sm_count() + blocks - 1) / blocks;
+    splits = splits < tiles ? splits : tiles;
+    return splits < 1 ? 1 : splits > kMaxSplits ? kMaxSplits : (int)splits;
+}
+size_t part_bytes(const RowsParams &p) { return align_up((size_t)p.tokens.total * p.hq * p.slots * (p.d + 2) * sizeof(float), 256); }
+
+int check_room(const rkv_desc_t *d, size_t bytes)
+{
+    if (bytes == 0) return RKV_OK;
+    if (!d->workspace || d->workspace_bytes < bytes || (reinterpret_cast<uintptr_t>(d->workspace) & 255u)) return RKV_ERR_WORKSPACE;
+    return RKV_OK;
+}
+
+// What a descriptor says about the rows' kernels.
+void fill_rows(const rkv_desc_t *d, int cap, RowsParams *p)
+{
+    p->hkv = d->n_kv_heads;
+    p->hq = d->n_q_heads;
+    p->group = d->n_q_heads / d->n_kv_heads;
+    p->d = d->head_dim;
+    p->cap = cap;
+    p->block_table = d->block_table;
+    p->pool_pages = d->pool_pages;
+    p->status = d->device_status;
+    p->wait_cycles = d->wait_limit_cycles > 0 ? (long long)d->wait_limit_cycles : sm100_default_wait_cycles();
+    p->splits = p->slots = 1;
+}
+
+int plan_window(const rkv_desc_t *d, int budget, int buffer, const rkv_tokens_t *tokens, int window, int sinks, RowsParams *p, size_t *bytes)
+{
+    int rc = check_cache(d, budget, buffer);
+    if (rc != RKV_OK) return rc;
+    *p = RowsParams{};
+    if ((rc = check_tokens(d, tokens, &p->tokens)) != RKV_OK) return rc;
+    if (window < 0 || sinks < 0) return RKV_ERR_INVALID_ARG;
+    const long long rows = (long long)tokens->longest * (d->n_q_heads / d->n_kv_heads);
+    if (rows > (1ll << 30) || (rows + kSimtRows - 1) / kSimtRows * d->n_kv_heads * d->batch > (1ll << 28)) return RKV_ERR_UNSUPPORTED;
+    fill_rows(d, budget + buffer, p);
+    p->causal = 1;
+    p->window = window;
+    p->sinks = sinks;
+    p->splits = p->slots = simt_splits(*p);
+    *bytes = p->slots > 1 ? part_bytes(*p) : 0;
+    return RKV_OK;
+}
+
+int check_prefix(const rkv_desc_t *d, const rkv_prefix_t *x)
+{
+    if (!x || x->count < 1 || d->batch % x->count != 0 || x->rows < 1) return RKV_ERR_INVALID_ARG;
+    if (x->rows > RKV_MAX_ROWS) return RKV_ERR_UNSUPPORTED;
+    if (x->table && (x->rows % kTile != 0 || x->pages < 1 || x->pages > (1ll << 23) || (reinterpret_cast<uintptr_t>(x->table) & 3u)))
+        return RKV_ERR_INVALID_ARG;
+    return RKV_OK;
+}
+
+// shared: the prefixes' rows; own: the sequences'.  Both leave partial results, side by side in a row's slots.
+int plan_prefix(const rkv_desc_t *d, int budget, int buffer, const rkv_prefix_t *x, RowsParams *shared, RowsParams *own, size_t *bytes)
+{
+    int rc = check_cache(d, budget, buffer);
+    if (rc != RKV_OK || (rc = check_prefix(d, x)) != RKV_OK) return rc;
+    if ((long long)d->batch * d->n_q_heads > (1ll << 28)) return RKV_ERR_UNSUPPORTED;
+    *shared = RowsParams{};
+    *own = RowsParams{};
+    fill_rows(d, x->rows, shared);
+    shared->block_table = x->table;
+    shared->pool_pages = x->pages;
+    shared->tokens = TokenMap{nullptr, x->count, d->batch, d->batch / x->count};
+    fill_rows(d, budget + buffer, own);
+    own->tokens = TokenMap{nullptr, d->batch, d->batch, 1};
+    shared->splits = simt_splits(*shared);
+    own->splits = simt_splits(*own);
+    own->slot = shared->splits;
+    shared->slots = own->slots = shared->splits + own->splits;
+    *bytes = part_bytes(*own);
+    return RKV_OK;
+}
+
 }  // namespace
 }  // namespace rkv
 
@@ -84,6 +175,76 @@ int rkv_append_rotary(const rkv_desc_t *d, void *k_cache, void *v_cache, const v
     p.status = d->device_status;
     const cudaError_t e = launch_append_rotary(p, d->dtype, static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? RKV_OK : cuda_fail(e, "rotated append launch");
+}
+
+size_t rkv_window_workspace_bytes(const rkv_desc_t *d, int32_t budget, int32_t buffer, const rkv_tokens_t *tokens, int32_t window,
+                                  int32_t sinks)
+{
+    RowsParams p;
+    size_t bytes = 0;
+    return plan_window(d, budget, buffer, tokens, window, sinks, &p, &bytes) == RKV_OK ? bytes : 0;
+}
+
+int rkv_window_attention(const rkv_desc_t *d, const void *k_cache, const void *v_cache, const void *q, const int32_t *seq_lens, void *out,
+                         int32_t budget, int32_t buffer, const rkv_tokens_t *tokens, int32_t window, int32_t sinks, void *stream)
+{
+    RowsParams p;
+    size_t bytes = 0;
+    int rc = plan_window(d, budget, buffer, tokens, window, sinks, &p, &bytes);
+    if (rc != RKV_OK) return rc;
+    if (!k_cache || !v_cache || !q || !seq_lens || !out) return RKV_ERR_INVALID_ARG;
+    if (!aligned16(k_cache) || !aligned16(v_cache) || !aligned16(q) || !aligned16(out)) return RKV_ERR_INVALID_ARG;
+    if (reinterpret_cast<uintptr_t>(seq_lens) & 3u) return RKV_ERR_INVALID_ARG;
+    const size_t esz = d->dtype == RKV_F32 ? 4 : 2;
+    p.q_stride = row_stride(tokens->q_stride, d->n_q_heads, d->head_dim, esz);
+    p.out_stride = row_stride(tokens->out_stride, d->n_q_heads, d->head_dim, esz);
+    if (!p.q_stride || !p.out_stride) return RKV_ERR_INVALID_ARG;
+    if ((rc = check_room(d, bytes)) != RKV_OK) return rc;
+    if (tokens->total == 0) return RKV_OK;
+    p.q = q;
+    p.k = k_cache;
+    p.v = v_cache;
+    p.lens = seq_lens;
+    p.out = out;
+    p.part = bytes ? static_cast<float *>(d->workspace) : nullptr;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    cudaError_t e = launch_rows_simt(p, d->dtype, s);
+    if (e == cudaSuccess && p.part) e = launch_rows_merge(p, d->dtype, s);
+    return e == cudaSuccess ? RKV_OK : cuda_fail(e, "window attention launch");
+}
+
+size_t rkv_prefix_workspace_bytes(const rkv_desc_t *d, int32_t budget, int32_t buffer, const rkv_prefix_t *prefix)
+{
+    RowsParams shared, own;
+    size_t bytes = 0;
+    return plan_prefix(d, budget, buffer, prefix, &shared, &own, &bytes) == RKV_OK ? bytes : 0;
+}
+
+int rkv_prefix_attention(const rkv_desc_t *d, const void *k_cache, const void *v_cache, const void *q_new, const int32_t *seq_lens, void *out,
+                         int32_t budget, int32_t buffer, const rkv_prefix_t *prefix, void *stream)
+{
+    RowsParams shared, own;
+    size_t bytes = 0;
+    int rc = plan_prefix(d, budget, buffer, prefix, &shared, &own, &bytes);
+    if (rc != RKV_OK) return rc;
+    if (!k_cache || !v_cache || !q_new || !seq_lens || !out || !prefix->k || !prefix->v || !prefix->lens) return RKV_ERR_INVALID_ARG;
+    for (const void *x : {k_cache, v_cache, q_new, (const void *)out, prefix->k, prefix->v})
+        if (!aligned16(x)) return RKV_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(seq_lens) | reinterpret_cast<uintptr_t>(prefix->lens)) & 3u) return RKV_ERR_INVALID_ARG;
+    if ((rc = check_room(d, bytes)) != RKV_OK) return rc;
+    shared.k = prefix->k, shared.v = prefix->v, shared.lens = prefix->lens;
+    own.k = k_cache, own.v = v_cache, own.lens = seq_lens;
+    for (RowsParams *p : {&shared, &own}) {
+        p->q = q_new;
+        p->out = out;
+        p->q_stride = p->out_stride = (long long)d->n_q_heads * d->head_dim;
+        p->part = static_cast<float *>(d->workspace);
+    }
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    cudaError_t e = launch_rows_simt(shared, d->dtype, s);
+    if (e == cudaSuccess) e = launch_rows_simt(own, d->dtype, s);
+    if (e == cudaSuccess) e = launch_rows_merge(own, d->dtype, s);
+    return e == cudaSuccess ? RKV_OK : cuda_fail(e, "prefix attention launch");
 }
 
 }  // extern "C"

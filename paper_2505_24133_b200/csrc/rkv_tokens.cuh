@@ -42,4 +42,51 @@ struct RotaryParams {
 };
 cudaError_t launch_append_rotary(RotaryParams p, int dtype, cudaStream_t s);
 
+// ---- attention of many query rows: "problems" (sequences, or prefixes), each a run of query tokens over one cache ----------------------
+// The rows of a problem and KV head are its tokens' G query heads, token after token: row r is head r % G of token r / G.
+struct RowsParams {
+    const void *q;                  // [total][hq][d], q_stride elements from token to token
+    long long q_stride, out_stride;
+    const void *k, *v;              // [count][hkv][cap][d], or pools
+    const int32_t *lens;            // [count]
+    const int32_t *block_table;
+    long long pool_pages;
+    TokenMap tokens;                // count = problems
+    int hkv, hq, group, d, cap;
+    int causal, window, sinks;      // causal: token t of n stands in row len - n + t and sees rows up to its own; else every token sees all rows
+    int splits, slot, slots;        // blocks that share a row tile's keys; their partial results are slots slot .. of the rows' `slots`
+    float *part;                    // [total * hq][slots][d + 2]: weighted sum, maximum (base 2), sum of weights; null: `out` is written
+    void *out;
+    int32_t *status;
+    long long wait_cycles;
+};
+// The key tiles of 128 rows that tokens t0 .. t1 of a problem look at: the first `sink_tiles`, then those from `first` on.
+struct KeyTiles {
+    int sink_tiles, first, count;
+    int lo, hi, sinks;              // rows seen by some of the tokens: [0, sinks) and [lo, hi)
+    __device__ __forceinline__ int tile(int i) const { return i < sink_tiles ? i : first + i - sink_tiles; }
+    __device__ __forceinline__ bool wanted(int row) const { return row < sinks || (row >= lo && row < hi); }
+};
+__device__ __forceinline__ KeyTiles key_tiles(int causal, int window, int sinks, int len, int n, int t0, int t1)
+{
+    KeyTiles k;
+    k.hi = causal ? len - n + t1 + 1 : len;
+    k.lo = causal && window > 0 ? max(0, len - n + t0 + 1 - window) : 0;
+    k.sinks = causal && window > 0 ? min(sinks, k.hi) : 0;
+    k.first = k.lo / kTile;
+    k.sink_tiles = min((k.sinks + kTile - 1) / kTile, k.first);
+    k.count = k.sink_tiles + (k.hi + kTile - 1) / kTile - k.first;
+    if (k.hi <= 0) k.count = 0;
+    return k;
+}
+// Rows of a cache: where 128-row tile t of a head starts, or -1 for a page that does not exist.
+__device__ __forceinline__ long long rows_tile_start(const RowsParams &p, int head, int t)
+{
+    if (!p.block_table) return (long long)head * p.cap + (long long)t * kTile;
+    const int page = p.block_table[(size_t)head * (p.cap / kTile) + t];
+    return page < 0 || page >= p.pool_pages ? -1 : (long long)page * kTile;
+}
+cudaError_t launch_rows_simt(const RowsParams &p, int dtype, cudaStream_t s);
+cudaError_t launch_rows_merge(const RowsParams &p, int dtype, cudaStream_t s);
+
 }  // namespace rkv

@@ -1,0 +1,183 @@
+"""rkv_prefix_attention on the GPU against the plain form in 64 bits."""
+import pytest
+import torch
+
+from tokens_util import TYPES, WIDE, attention, attention_tolerance, descriptor, random_rows, to_pages
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def rkv():
+    from paper_2505_24133_b200 import build as b
+    b.build()
+    import paper_2505_24133_b200 as r
+    assert r.lib() is not None
+    return r
+
+
+class Setup:
+    """Rows beyond the lengths are NaN."""
+
+    def __init__(self, rkv, dtype, d, hkv, hq, lens, prefix_lens, cap, rows, seed=41, paged=False):
+        gen = torch.Generator(device="cuda").manual_seed(seed)
+        self.rkv, self.d, self.hkv, self.hq, self.cap = rkv, d, hkv, hq, cap
+        self.lens, self.plens = list(lens), list(prefix_lens)
+        B, n = len(lens), len(prefix_lens)
+        self.k, self.v = (random_rows((B, hkv, cap, d), dtype, gen, lens) for _ in range(2))
+        self.pk, self.pv = (random_rows((n, hkv, rows, d), dtype, gen, prefix_lens) for _ in range(2))
+        self.plain = [x.clone() for x in (self.k, self.v, self.pk, self.pv)]
+        self.table = self.ptable = None
+        if paged:
+            self.k, self.table = to_pages(self.k, gen)
+            self.v = self.other_pool(self.plain[1], self.k, self.table)
+            self.pk, self.ptable = to_pages(self.pk, gen)
+            self.pv = self.other_pool(self.plain[3], self.pk, self.ptable)
+        self.q = torch.randn(B, hq, d, generator=gen, device="cuda").to(WIDE[dtype])
+        self.out = torch.full_like(self.q, 7.0)
+        self.seq = torch.tensor(lens, dtype=torch.int32, device="cuda")
+        self.pseq = torch.tensor(prefix_lens, dtype=torch.int32, device="cuda")
+        self.status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        self.desc = descriptor(rkv, B, hkv, hq, d, dtype, self.status, self.table, self.k.shape[0] if paged else 0)
+        self.prefix = rkv.rkv_prefix(self.pk, self.pv, self.pseq, self.ptable)
+        n = rkv.rkv_prefix_workspace_bytes(self.desc, cap - 1, 1, self.prefix)
+        self.room = torch.full((max(n, 256),), 0xFF, dtype=torch.uint8, device="cuda")
+        self.desc.workspace, self.desc.workspace_bytes = self.room.data_ptr(), n
+
+    @staticmethod
+    def other_pool(x, like, table):
+        pool = torch.empty_like(like)
+        pool.view(torch.uint8).fill_(0x7F if x.dtype == torch.float8_e4m3fn else 0xFF)
+        pool.view(torch.uint8)[table.flatten().long()] = x.contiguous().view(torch.uint8).view(table.numel(), 128, -1)
+        return pool
+
+    def call(self, stream=None):
+        return self.rkv.rkv_prefix_attention(self.desc, self.k, self.v, self.q, self.seq, self.out, self.cap - 1, 1, self.prefix, stream)
+
+    def check(self, bad=()):
+        k, v, pk, pv = self.plain
+        G, per = self.hq // self.hkv, len(self.lens) // len(self.plens)
+        for b, L in enumerate(self.lens):
+            P = self.plens[b // per]
+            L = 0 if b in bad else L
+            for h in range(self.hkv):
+                keys = torch.cat([pk[b // per, h, :P].float(), k[b, h, :L].float()])
+                values = torch.cat([pv[b // per, h, :P].float(), v[b, h, :L].float()])
+                got = self.out[b:b + 1, h * G:(h + 1) * G].double()
+                if P + L == 0:
+                    assert (got == 0).all()
+                    continue
+                ref, size = attention(self.q[b:b + 1, h * G:(h + 1) * G], keys, values, torch.ones(1, P + L, dtype=torch.bool, device="cuda"))
+                assert torch.isfinite(got).all(), (b, h)
+                over = float(((got - ref).abs() - attention_tolerance(ref, size, P + L, self.d, self.out.dtype)).max())
+                assert over <= 0, (b, h, over)
+        assert int(self.status.item()) == (1 if bad else 0)
+
+    def run(self, bad=()):
+        assert self.call() == 0
+        torch.cuda.synchronize()
+        self.check(bad)
+        return self
+
+
+SHAPES = [("bf16", 128), ("bf16", 64), ("bf16", 256), ("fp8", 128), ("fp8", 64), ("f32", 128), ("f32", 64), ("f32", 256)]
+
+
+@pytest.mark.parametrize("dtype,d", SHAPES)
+@pytest.mark.parametrize("paged", [False, True])
+def test_lengths(rkv, dtype, d, paged):
+    """Prefixes of no row, one row and odd lengths; own caches that are empty, hold one row, are full."""
+    Setup(rkv, dtype, d, 2, 8, [0, 1, 127, 256, 0, 129, 5, 200], [300, 0, 1, 257], 256, 384, paged=paged).run()
+
+
+@pytest.mark.parametrize("hkv,hq", [(1, 1), (2, 6), (1, 5), (2, 14), (1, 8), (1, 16), (1, 100), (1, 130)])
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("fp8", 128), ("f32", 128)])
+@pytest.mark.parametrize("batch", [1, 3, 50])
+def test_head_layouts_and_batches(rkv, dtype, d, hkv, hq, batch):
+    """One row of queries up to many row tiles per prefix."""
+    Setup(rkv, dtype, d, hkv, hq, [(37 * b) % 300 for b in range(batch)], [333], 300, 400).run()
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("fp8", 128), ("f32", 128)])
+@pytest.mark.parametrize("batch,prefixes,rows,cap", [(2, 1, 6000, 200), (16, 2, 5000, 4500), (48, 3, 2000, 1000), (64, 64, 300, 300), (200, 1, 130, 64)])
+def test_long_prefixes_and_many_samples(rkv, dtype, d, batch, prefixes, rows, cap):
+    Setup(rkv, dtype, d, 2, 8, [(cap * (b + 1)) // batch for b in range(batch)], [max(0, rows - 7 * p) for p in range(prefixes)], cap, rows).run()
+
+
+def test_bad_lengths_count_as_none(rkv):
+    s = Setup(rkv, "bf16", 128, 2, 8, [50, 301, -1, 20], [300], 300, 300)
+    s.run(bad=(1, 2))
+    s = Setup(rkv, "bf16", 128, 2, 8, [50, 30, 0, 20], [100, 100], 300, 300)
+    s.pseq.copy_(torch.tensor([301, -1], dtype=torch.int32))
+    s.plens = [0, 0]
+    assert s.call() == 0
+    torch.cuda.synchronize()
+    assert int(s.status.item()) == 1
+    s.status.zero_()
+    s.check()
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("fp8", 128), ("f32", 128)])
+def test_pages_that_do_not_exist_count_as_zeros(rkv, dtype, d):
+    s = Setup(rkv, dtype, d, 1, 4, [200, 256], [256], 256, 256, paged=True)
+    s.ptable[0, 0, 0], s.table[1, 0, 1] = s.pk.shape[0], -3
+    assert s.call() == 0
+    torch.cuda.synchronize()
+    assert int(s.status.item()) == 1
+    for x in s.plain[:2]:
+        x.view(torch.uint8)[1, :, 128:] = 0
+    for x in s.plain[2:]:
+        x.view(torch.uint8)[0, :, :128] = 0
+    s.status.zero_()
+    s.check()
+
+
+def test_one_prefix_equals_each_sequence_with_the_rows_of_its_own(rkv):
+    """The same rows stored in front of every sequence's own: the decode attention over them agrees to the rounding of the output and weights."""
+    s = Setup(rkv, "bf16", 128, 2, 8, [40, 200, 0], [300], 256, 300).run()
+    k, v, pk, pv = s.plain
+    cap = 640
+    joined = []
+    for own, shared in ((k, pk), (v, pv)):
+        x = torch.zeros(3, 2, cap, 128, dtype=torch.bfloat16, device="cuda")
+        x[:, :, :300] = shared
+        for b, L in enumerate(s.lens):
+            x[b, :, 300:300 + L] = own[b, :, :L]
+        joined.append(x)
+    desc = descriptor(rkv, 3, 2, 8, 128, "bf16", s.status)
+    room = torch.empty(rkv.rkv_decode_workspace_bytes(desc, cap - 1, 1), dtype=torch.uint8, device="cuda")
+    desc.workspace, desc.workspace_bytes = room.data_ptr(), room.numel()
+    out = torch.empty(3, 8, 128, device="cuda")
+    lens = torch.tensor([300 + L for L in s.lens], dtype=torch.int32, device="cuda")
+    assert rkv.rkv_decode_attention(desc, joined[0], joined[1], s.q, lens, out, cap - 1, 1) == 0
+    torch.cuda.synchronize()
+    # values N(0, 1), at most 500 of them: |v| < 6; the weights' and the output's rounding are half a bf16 step each
+    assert float((out - s.out.float()).abs().max()) <= 2.0 ** -8 * (6.0 + 6.0)
+
+
+def test_another_stream_and_a_captured_graph(rkv):
+    s = Setup(rkv, "bf16", 128, 2, 8, [40, 200, 0, 130], [300, 100], 256, 300)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    assert s.call(side) == 0
+    torch.cuda.synchronize()
+    s.check()
+    want = s.out.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        assert s.call() == 0
+    for _ in range(2):
+        s.out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(s.out, want)
+    # other lengths, the same graph
+    s.lens, s.plens = [10, 0, 256, 1], [1, 300]
+    s.seq.copy_(torch.tensor(s.lens, dtype=torch.int32))
+    s.pseq.copy_(torch.tensor(s.plens, dtype=torch.int32))
+    for x, n in ((s.k, s.lens), (s.v, s.lens), (s.pk, s.plens), (s.pv, s.plens)):
+        x.normal_()
+    s.plain = [x.clone() for x in (s.k, s.v, s.pk, s.pv)]
+    graph.replay()
+    torch.cuda.synchronize()
+    s.check()

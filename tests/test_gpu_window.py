@@ -1,0 +1,302 @@
+"""rkv_window_attention on the GPU against the plain form in 64 bits."""
+import pytest
+import torch
+
+from tokens_util import TYPES, WIDE, attention, attention_tolerance, descriptor, random_rows, to_pages
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def rkv():
+    from paper_2505_24133_b200 import build as b
+    b.build()
+    import paper_2505_24133_b200 as r
+    assert r.lib() is not None
+    return r
+
+
+def visible(length, n, window, sinks):
+    at = torch.arange(length - n, length, device="cuda")[:, None]
+    j = torch.arange(length, device="cuda")[None]
+    return (j <= at) & ((at - j < window) | (j < sinks) if window else (j <= at))
+
+
+class Setup:
+    """Rows that no new token sees are NaN, and pages of nothing but such rows have no valid entry in the block table."""
+
+    def __init__(self, rkv, dtype, d, hkv, hq, lens, new, cap, window, sinks, seed=31, paged=False, strided=False, behind=0, offsets=True,
+                 longest=None):
+        gen = torch.Generator(device="cuda").manual_seed(seed)
+        self.rkv, self.d, self.hkv, self.hq, self.cap = rkv, d, hkv, hq, cap
+        self.lens, self.new, self.window, self.sinks = list(lens), list(new), window, sinks
+        B, total = len(lens), sum(new) + behind
+        self.k, self.v = random_rows((B, hkv, cap, d), dtype, gen), random_rows((B, hkv, cap, d), dtype, gen)
+        self.k0, self.v0 = self.k.clone(), self.v.clone()
+        unseen = torch.ones(B, cap, dtype=torch.bool, device="cuda")
+        for b, (L, n) in enumerate(zip(lens, new)):
+            if 0 < n <= L <= cap:
+                unseen[b, :L] = ~visible(L, n, window, sinks).any(0)
+        mark = 0x7F if dtype == "fp8" else 0xFF
+        for x in (self.k, self.v):
+            raw = x.view(torch.uint8).view(B, hkv, cap, -1)
+            raw[unseen[:, None].expand(B, hkv, cap)] = mark
+        self.table = None
+        if paged:
+            self.k, self.table = to_pages(self.k, gen)
+            pool = torch.empty_like(self.k)
+            pool.view(torch.uint8).fill_(mark)
+            raw = self.v.view(torch.uint8).view(B * hkv * cap // 128, 128, -1)
+            pool.view(torch.uint8)[self.table.flatten().long()] = raw
+            self.v = pool
+            gone = unseen.view(B, 1, cap // 128, 128).all(-1).expand_as(self.table)
+            self.table[gone] = -7
+        wide = WIDE[dtype]
+        rows = torch.randn(total, hq + 3, d, generator=gen, device="cuda").to(wide)
+        self.q = rows[:, :hq] if strided else rows[:, :hq].contiguous()
+        self.out_rows = torch.full((total, hq + (2 if strided else 0), d), 7.0, device="cuda", dtype=wide)
+        self.out = self.out_rows[:, :hq]
+        self.seq = torch.tensor(lens, dtype=torch.int32, device="cuda")
+        off = torch.tensor([sum(new[:b]) for b in range(B + 1)], dtype=torch.int32, device="cuda")
+        self.offsets = off if offsets else None
+        stride = dict(q_stride=self.q.stride(0), out_stride=self.out.stride(0)) if strided else {}
+        self.tokens = rkv.rkv_tokens(total, longest or max(max(new), 1), self.offsets, **stride)
+        self.status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        self.desc = descriptor(rkv, B, hkv, hq, d, dtype, self.status, self.table, self.k.shape[0] if paged else 0)
+        self.workspace(self.desc)
+
+    def workspace(self, desc):
+        n = self.rkv.rkv_window_workspace_bytes(desc, self.cap - 1, 1, self.tokens, self.window, self.sinks)
+        self.room = torch.full((max(n, 256),), 0xFF, dtype=torch.uint8, device="cuda")
+        desc.workspace, desc.workspace_bytes = self.room.data_ptr(), n
+        return n
+
+    def call(self, stream=None):
+        return self.rkv.rkv_window_attention(self.desc, self.k, self.v, self.q, self.seq, self.out, self.cap - 1, 1, self.tokens, self.window,
+                                             self.sinks, stream)
+
+    def check(self, refused=()):
+        first, wide = 0, self.out.dtype
+        G = self.hq // self.hkv
+        for b, (L, n) in enumerate(zip(self.lens, self.new)):
+            t = slice(first, first + n)
+            first += n
+            if b in refused:
+                assert (self.out[t] == 0).all()
+                continue
+            if n == 0:
+                continue
+            seen = visible(L, n, self.window, self.sinks)
+            for h in range(self.hkv):
+                ref, size = attention(self.q[t, h * G:(h + 1) * G], self.k0[b, h, :L], self.v0[b, h, :L], seen)
+                got = self.out[t, h * G:(h + 1) * G].double()
+                assert torch.isfinite(got).all(), (b, h)
+                over = float(((got - ref).abs() - attention_tolerance(ref, size, min(L, (self.window or L) + self.sinks), self.d, wide)).max())
+                assert over <= 0, (b, h, over)
+        assert (self.out[first:] == 7.0).all() and (self.out_rows[:, self.hq:] == 7.0).all()
+        assert int(self.status.item()) == (1 if refused else 0)
+
+    def run(self, refused=()):
+        assert self.call() == 0
+        torch.cuda.synchronize()
+        self.check(refused)
+        return self
+
+
+SHAPES = [("bf16", 128), ("bf16", 64), ("bf16", 256), ("fp8", 128), ("fp8", 64), ("f32", 128), ("f32", 64), ("f32", 256)]
+
+
+@pytest.mark.parametrize("dtype,d", SHAPES)
+@pytest.mark.parametrize("window,sinks", [(0, 0), (1, 0), (1, 3), (100, 4), (128, 0), (129, 128), (300, 130), (4000, 5)])
+def test_one_token_per_sequence(rkv, dtype, d, window, sinks):
+    """One cached row, lengths on both sides of a tile's and the window's border, a full cache."""
+    lens = [1, 2, 127, 128, 129, 300, 431, 640]
+    Setup(rkv, dtype, d, 2, 8, lens, [1] * 8, 640, window, sinks, offsets=False).run()
+
+
+@pytest.mark.parametrize("dtype,d", SHAPES)
+@pytest.mark.parametrize("window,sinks,paged", [(0, 0, False), (0, 9, True), (1, 1, True), (60, 4, False), (200, 130, True), (257, 0, True)])
+def test_ragged_prompts(rkv, dtype, d, window, sinks, paged):
+    """Prompts and pieces of prompts of 0 to 300 tokens over caches that hold more, or nothing else."""
+    new = [0, 1, 5, 128, 129, 300, 0, 33]
+    lens = [0, 1, 400, 128, 640, 300, 50, 513]
+    Setup(rkv, dtype, d, 2, 8, lens, new, 640, window, sinks, paged=paged, strided=True, behind=3).run()
+
+
+@pytest.mark.parametrize("hkv,hq", [(1, 1), (3, 3), (2, 6), (1, 5), (2, 12), (1, 7), (2, 16), (1, 16), (1, 48), (1, 100), (1, 130)])
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("fp8", 128), ("f32", 128)])
+def test_head_layouts(rkv, dtype, d, hkv, hq):
+    Setup(rkv, dtype, d, hkv, hq, [40, 259], [40, 77], 300, 50, 4).run()
+    Setup(rkv, dtype, d, hkv, hq, [40, 259], [1, 1], 300, 150, 4, offsets=False).run()
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("fp8", 128), ("bf16", 64), ("f32", 128)])
+@pytest.mark.parametrize("n,window,sinks", [(1, 0, 0), (1, 2500, 4), (2, 0, 0), (3, 3000, 200), (40, 0, 0), (700, 1500, 4)])
+def test_long_caches(rkv, dtype, d, n, window, sinks):
+    """Few rows over many keys: the keys are split between blocks."""
+    Setup(rkv, dtype, d, 1, 4, [5000, 4999], [n, n], 5120, window, sinks, offsets=n > 1, paged=True).run()
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("fp8", 128), ("bf16", 64), ("f32", 128)])
+def test_long_prompts(rkv, dtype, d):
+    """Every piece of a prompt of 1500 tokens, whole and with a window."""
+    for window, sinks in ((0, 0), (333, 4)):
+        Setup(rkv, dtype, d, 2, 8, [1500, 900], [1500, 900], 1536, window, sinks).run()
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("fp8", 128), ("f32", 128)])
+@pytest.mark.parametrize("step", [True, False])
+def test_bad_lengths_give_zeros(rkv, dtype, d, step):
+    n = 1 if step else 4
+    s = Setup(rkv, dtype, d, 2, 4, [-1, 100, 301, n - 1, 300], [n] * 5, 300, 50, 4, offsets=not step)
+    s.run(refused=(0, 2, 3))
+
+
+def test_bad_offsets_write_nothing(rkv):
+    s = Setup(rkv, "bf16", 128, 2, 4, [50, 60, 70], [4, 4, 4], 300, 50, 4)
+    s.offsets.copy_(torch.tensor([0, 4, 11, 12], dtype=torch.int32))          # more tokens than the call said
+    assert s.call() == 0
+    torch.cuda.synchronize()
+    assert (s.out[4:11] == 7.0).all() and int(s.status.item()) == 1
+    assert (s.out[:4] != 7.0).any() and (s.out[11:] != 7.0).any()
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("fp8", 128), ("bf16", 64), ("f32", 128)])
+@pytest.mark.parametrize("n", [1, 30])
+def test_pages_that_do_not_exist_count_as_zeros(rkv, dtype, d, n):
+    s = Setup(rkv, dtype, d, 1, 2, [256, 256], [n, n], 256, 0, 0, paged=True)
+    s.table[0, 0, 1], s.table[1, 0, 0] = -1, 1 << 30
+    assert s.call() == 0
+    torch.cuda.synchronize()
+    assert int(s.status.item()) == 1
+    s.k0.view(torch.uint8)[0, :, 128:] = 0
+    s.v0.view(torch.uint8)[0, :, 128:] = 0
+    s.k0.view(torch.uint8)[1, :, :128] = 0
+    s.v0.view(torch.uint8)[1, :, :128] = 0
+    s.status.zero_()
+    s.check()
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 128)])
+def test_large_scores(rkv, dtype, d):
+    """Scores whose exponentials overflow and underflow 32 bits, growing and falling along the cache."""
+    for sign in (1.0, -1.0):
+        s = Setup(rkv, dtype, d, 1, 4, [700, 640], [200, 1], 700, 0, 0)
+        ramp = sign * torch.linspace(-8, 8, 700, device="cuda")
+        for x in (s.k, s.k0):
+            x.copy_((ramp[:, None] * torch.ones(d, device="cuda")).to(x.dtype).expand_as(x))
+        s.q.copy_((s.q.float() * 0.25 + 4.0).to(s.q.dtype))
+        assert s.call() == 0
+        torch.cuda.synchronize()
+        first = 0
+        for b, (L, n) in enumerate(zip(s.lens, s.new)):
+            # scores up to 8 * 4 * 128 / sqrt(128) = 362 (bf16 products are exact, sums off by 130 * 2^-24 * 362 < 0.003)
+            ref, size = attention(s.q[first:first + n], s.k0[b, 0, :L], s.v0[b, 0, :L], visible(L, n, 0, 0))
+            tol = (ref.abs() + size) * 2.0 ** -8 * (1 if dtype == "bf16" else 0) + size * 2 * (0.003 + 2.0 ** -12)
+            assert torch.isfinite(s.out[first:first + n]).all()
+            assert ((s.out[first:first + n].double() - ref).abs() <= tol).all()
+            first += n
+
+
+def test_rows_beyond_32_bits(rkv):
+    """The last head of a cache of more than 2^31 elements."""
+    hkv, cap, d = 20, 1 << 20, 128
+    k = torch.zeros(1, hkv, cap, d, dtype=torch.float8_e4m3fn, device="cuda")
+    v = torch.zeros_like(k)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    for x in (k, v):
+        x[0, :, cap - 300:] = torch.randn(hkv, 300, d, generator=gen, device="cuda").to(x.dtype)
+    for n in (1, 5):
+        q = torch.randn(n, hkv, d, generator=gen, device="cuda").to(torch.bfloat16)
+        out = torch.zeros_like(q)
+        seq = torch.tensor([cap], dtype=torch.int32, device="cuda")
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        desc = descriptor(rkv, 1, hkv, hkv, d, "fp8", status)
+        tokens = rkv.rkv_tokens(n, n)
+        room = torch.empty(rkv.rkv_window_workspace_bytes(desc, cap - 1, 1, tokens, 200, 0) or 256, dtype=torch.uint8, device="cuda")
+        desc.workspace, desc.workspace_bytes = room.data_ptr(), room.numel()
+        assert rkv.rkv_window_attention(desc, k, v, q, seq, out, cap - 1, 1, tokens, 200, 0) == 0
+        torch.cuda.synchronize()
+        assert int(status.item()) == 0
+        seen = visible(cap, n, 200, 0)[:, cap - 300:]
+        for h in range(hkv):
+            ref, size = attention(q[:, h:h + 1], k[0, h, cap - 300:].float(), v[0, h, cap - 300:].float(), seen)
+            assert ((out[:, h:h + 1].double() - ref).abs() <= attention_tolerance(ref, size, 200, d, torch.bfloat16)).all(), h
+
+
+def test_another_stream_and_captured_graphs(rkv):
+    """Two captured calls of different shapes that share a workspace, replayed in turn, give what eager calls gave."""
+    a = Setup(rkv, "bf16", 128, 2, 8, [900, 800], [1, 1], 1024, 0, 0, offsets=False)
+    c = Setup(rkv, "bf16", 128, 2, 8, [900, 800], [40, 7], 1024, 300, 4, seed=32)
+    n = max(a.room.numel(), c.room.numel())
+    room = torch.empty(n, dtype=torch.uint8, device="cuda")
+    for x in (a, c):
+        x.desc.workspace, x.desc.workspace_bytes = room.data_ptr(), n
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for x in (a, c):
+        assert x.call(side) == 0
+    torch.cuda.synchronize()
+    a.check(), c.check()
+    want = a.out.clone(), c.out.clone()
+    graphs = []
+    for x in (a, c):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            assert x.call() == 0
+        graphs.append(g)
+    for _ in range(2):
+        a.out.zero_(), c.out.zero_()
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(a.out, want[0]) and torch.equal(c.out, want[1])
+
+
+def test_append_then_attend_like_a_decode_loop(rkv):
+    """A prompt, three decode steps and a compression: after each append the attention sees the rows that are there, rotated."""
+    from tokens_util import rotation_table
+    B, hkv, hq, d, budget, buffer, alpha = 2, 2, 8, 128, 128, 64, 8
+    cap = budget + buffer
+    comp = rkv.Compressor(B, hkv, hq, budget, buffer, alpha)
+    gen = torch.Generator(device="cuda").manual_seed(33)
+    draw = lambda *shape: torch.randn(*shape, generator=gen, device="cuda").to(torch.bfloat16)  # noqa: E731
+    k, v = (torch.full((B, hkv, cap, d), float("nan"), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    seq = torch.zeros(B, dtype=torch.int32, device="cuda")
+    position = torch.zeros(B, dtype=torch.int32, device="cuda")
+    table = rotation_table(1024, d)
+    prompts = [189, 150]
+    q_window = draw(B, hq, alpha, d)
+
+    def step(tokens, counts):
+        n = tokens.total
+        kn, vn, qn = draw(n, hkv, d), draw(n, hkv, d), draw(n, hq, d)
+        q, out = torch.empty_like(qn), torch.empty_like(qn)
+        assert rkv.rkv_append_rotary(comp.desc, k, v, kn, vn, seq, budget, buffer, tokens, rkv.rkv_rotary(table, d, position), qn, q) == 0
+        position.add_(torch.tensor(counts, dtype=torch.int32, device="cuda"))
+        room = torch.empty(rkv.rkv_window_workspace_bytes(comp.desc, budget, buffer, tokens, 100, 4) or 256, dtype=torch.uint8, device="cuda")
+        desc = descriptor(rkv, B, hkv, hq, d, "bf16", comp.status)
+        desc.workspace, desc.workspace_bytes = room.data_ptr(), room.numel()
+        assert rkv.rkv_window_attention(desc, k, v, q, seq, out, budget, buffer, tokens, 100, 4) == 0
+        torch.cuda.synchronize()
+        comp.check_status()
+        first = 0
+        for b, m in enumerate(counts):
+            L = int(seq[b])
+            for h in range(hkv):
+                heads = slice(h * 4, h * 4 + 4)
+                ref, size = attention(q[first:first + m, heads], k[b, h, :L], v[b, h, :L], visible(L, m, 100, 4))
+                over = (out[first:first + m, heads].double() - ref).abs() - attention_tolerance(ref, size, 104, d, torch.bfloat16)
+                assert float(over.max()) <= 0
+            first += m
+
+    step(rkv.rkv_tokens(sum(prompts), max(prompts), torch.tensor([0, 189, 339], dtype=torch.int32, device="cuda")), prompts)
+    for _ in range(3):
+        step(rkv.rkv_tokens(B, 1), [1, 1])
+    assert seq.tolist() == [192, 153]
+    comp.compress(k, v, q_window, seq)
+    torch.cuda.synchronize()
+    comp.check_status()
+    assert seq.tolist() == [budget, budget] and position.tolist() == [192, 153]
+    step(rkv.rkv_tokens(B, 1), [1, 1])                       # positions go on where they were, rows where the compression left them
+    assert seq.tolist() == [budget + 1, budget + 1] and position.tolist() == [193, 154]

@@ -84,3 +84,51 @@ def test_token_tensors_have_the_strides_they_are_said_to_have(rkv):
     with pytest.raises(AssertionError):                           # strided, but the call was not told
         rkv.rkv_append_rotary(d, None, None, qkv[:, :2], qkv[:, 2:4], None, 64, 32, rkv.rkv_tokens(4, 4), r, None, None, 0)
     assert rkv.rkv_append_rotary(d, None, None, qkv[:, :2], qkv[:, 2:4], None, 64, 32, t, r, None, None, 0) == 1
+
+
+@pytest.mark.parametrize("case,want", [
+    (dict(k_cache=None), 1), (dict(q=None), 1), (dict(out=None), 1), (dict(seq=None), 1), (dict(q=GOOD + 8), 1), (dict(out=GOOD + 4), 1),
+    (dict(seq=GOOD + 2), 1), (dict(window=-1), 1), (dict(sinks=-1), 1), (dict(budget=0), 1), (dict(budget=1 << 20), 2),
+    (dict(desc=dict(head_dim=96)), 2), (dict(desc=dict(n_q_heads=30)), 1), (dict(tokens=dict(q_stride=4100)), 1),
+    (dict(tokens=dict(out_stride=4095)), 1), (dict(tokens=dict(longest=0)), 1), (dict(tokens=dict(offsets=None)), 1),
+    (dict(desc=dict(block_table=GOOD, pool_pages=9)), 1), (dict(desc=dict(workspace=None)), 3), (dict(desc=dict(workspace=0x10010)), 3),
+    (dict(desc=dict(workspace_bytes=1024)), 3), (dict(tokens=dict(total=0)), 0),
+])
+def test_window_attention_refuses(rkv, case, want):
+    a = dict(k_cache=GOOD, v_cache=GOOD, q=GOOD, seq=GOOD, out=GOOD, budget=1000, buffer=1, window=100, sinks=4)
+    a.update({k: v for k, v in case.items() if k in a})
+    d = _desc(rkv, workspace=0x10000, workspace_bytes=1 << 40)
+    for k, v in case.get("desc", {}).items():
+        setattr(d, k, v)
+    t = _tokens(rkv, **case.get("tokens", {}))
+    assert rkv.rkv_window_attention(d, a["k_cache"], a["v_cache"], a["q"], a["seq"], a["out"], a["budget"], a["buffer"], t, a["window"],
+                                    a["sinks"], 0) == want
+
+
+@pytest.mark.parametrize("case,want", [
+    (dict(k_cache=None), 1), (dict(q=None), 1), (dict(out=GOOD + 8), 1), (dict(seq=GOOD + 1), 1), (dict(budget=0), 1),
+    (dict(prefix=dict(k=None)), 1), (dict(prefix=dict(v=GOOD + 4)), 1), (dict(prefix=dict(lens=None)), 1), (dict(prefix=dict(lens=GOOD + 2)), 1),
+    (dict(prefix=dict(count=0)), 1), (dict(prefix=dict(count=3)), 1), (dict(prefix=dict(rows=0)), 1), (dict(prefix=dict(rows=(1 << 20) + 1)), 2),
+    (dict(prefix=dict(table=GOOD, pages=4, rows=100)), 1), (dict(prefix=dict(table=GOOD, pages=0, rows=128)), 1),
+    (dict(prefix=dict(table=GOOD + 2, pages=4, rows=128)), 1), (dict(desc=dict(workspace=None)), 3), (dict(desc=dict(workspace_bytes=256)), 3),
+    (dict(desc=dict(dtype=5)), 2),
+])
+def test_prefix_attention_refuses(rkv, case, want):
+    a = dict(k_cache=GOOD, v_cache=GOOD, q=GOOD, seq=GOOD, out=GOOD, budget=1000, buffer=1)
+    a.update({k: v for k, v in case.items() if k in a})
+    d = _desc(rkv, workspace=0x10000, workspace_bytes=1 << 40)
+    for k, v in case.get("desc", {}).items():
+        setattr(d, k, v)
+    x = rkv.RkvPrefix(GOOD, GOOD, 2, 500, GOOD, None, 0)
+    for k, v in case.get("prefix", {}).items():
+        setattr(x, k, v)
+    assert rkv.rkv_prefix_attention(d, a["k_cache"], a["v_cache"], a["q"], a["seq"], a["out"], a["budget"], a["buffer"], x, 0) == want
+
+
+def test_workspace_sizes(rkv):
+    """Zero for what is refused, and of the window attention for calls that fill the GPU."""
+    d, t = _desc(rkv), _tokens(rkv)
+    assert rkv.rkv_window_workspace_bytes(d, 1000, 1, t, -1, 0) == 0 and rkv.rkv_window_workspace_bytes(_desc(rkv, head_dim=32), 1000, 1, t, 0, 0) == 0
+    assert rkv.rkv_window_workspace_bytes(_desc(rkv, batch=512), 1000, 1, rkv.rkv_tokens(512 * 64, 64), 0, 0) == 0
+    x = rkv.RkvPrefix(GOOD, GOOD, 2, 500, GOOD, None, 0)
+    assert rkv.rkv_prefix_workspace_bytes(d, 1000, 1, x) > 0 and rkv.rkv_prefix_workspace_bytes(_desc(rkv, batch=3), 1000, 1, x) == 0

@@ -80,3 +80,14 @@ def attention(q, keys, values, visible):
     total = w.sum(-1, keepdim=True)
     w = torch.where(total > 0, w / total.clamp_min(1e-300), 0.0)
     return torch.einsum("ngj,jd->ngd", w, values), torch.einsum("ngj,jd->ngd", w, values.abs())
+
+
+def attention_tolerance(ref, size, rows, d, out_type):
+    """Values N(0, 1).  A score's products are added up in fp32: off by at most (d + 2) 2^-24 sum |q k| / sqrt(d), and sum |q k| <= |q| |k|
+    < 2 d; the exponential adds 2^-20.  Such an error of every weight moves the result by twice it, relative to the weighted mean of |v|
+    (numerator and denominator); adding up `rows` weighted values adds rows 2^-24.  bf16 products round the weights (half a step of
+    bf16).  Then one rounding to the output's type."""
+    delta = (d + 2) * 2.0 ** -24 * 2 * d ** 0.5 + 2.0 ** -20
+    weights = 2.0 ** -8 if out_type == torch.bfloat16 else 0.0
+    inner = size * (2 * delta + rows * 2.0 ** -24 + weights)
+    return inner + (ref.abs() + inner) * HALF_STEP[out_type]
