@@ -13,6 +13,8 @@ int check_cache(const rkv_desc_t *d, int budget, int buffer)
     if (d->head_dim != 64 && d->head_dim != 128 && d->head_dim != 256) return RKV_ERR_UNSUPPORTED;
     if (d->dtype != RKV_BF16 && d->dtype != RKV_F32 && d->dtype != RKV_FP8_E4M3) return RKV_ERR_UNSUPPORTED;
     const long long cap = (long long)budget + buffer;
+    // (rows of all heads are numbered in 32 bits; so many would not fit the GPU's memory)
+    if (!d->block_table && (long long)d->batch * d->n_kv_heads * cap > 0x7fffffffll) return RKV_ERR_UNSUPPORTED;
     if (cap > RKV_MAX_ROWS || (long long)d->batch * d->n_kv_heads > (1ll << 24) || d->n_q_heads > (1 << 16)) return RKV_ERR_UNSUPPORTED;
     if (d->block_table) {
         if (cap % kTile != 0 || d->pool_pages < 1 || d->pool_pages > (1ll << 23)) return RKV_ERR_INVALID_ARG;
@@ -44,17 +46,32 @@ int sm_count()
     return device_sms(&dev, &sms) == cudaSuccess ? sms : 148;    // sizing only (no device here): the B200's count
 }
 
-// Query rows of 64 to a block: the tiles of 128 keys that such a block may come to are shared out until there are two waves of blocks (two to
-// an SM).
+// Splits of the blocks' key tiles.  `rows` query rows to a block, `resident` blocks on the GPU at a time: the shortest run, counted in
+// waves of blocks times the tiles of each and three more for its start and end; two more for the merge kernel.
 constexpr int kSimtRows = 64, kMaxSplits = 64;
-int simt_splits(const RowsParams &p)
+int rows_splits(const RowsParams &p, int tokens_per_block, long long resident)
 {
-    const long long blocks = ((long long)p.tokens.longest * p.group + kSimtRows - 1) / kSimtRows * p.hkv * p.tokens.count;
-    const long long seen = p.causal && p.window > 0 ? (long long)p.window + kSimtRows / p.group + 1 : p.cap;
-    const long long tiles = (seen < p.cap ? seen / kTile + 2 + (p.sinks + kTile - 1) / kTile : (p.cap + kTile - 1) / kTile);
-    long long splits = (4ll * sm_count() + blocks - 1) / blocks;
-    splits = splits < tiles ? splits : tiles;
-    return splits < 1 ? 1 : splits > kMaxSplits ? kMaxSplits : (int)splits;
+    const long long blocks = ((long long)p.tokens.longest + tokens_per_block - 1) / tokens_per_block * p.hkv * p.tokens.count;
+    const long long seen = p.causal && p.window > 0 ? (long long)p.window + tokens_per_block : p.cap;
+    const long long tiles = seen < p.cap ? seen / kTile + 2 + (p.sinks < p.cap ? (p.sinks + kTile - 1) / kTile : 0) : (p.cap + kTile - 1) / kTile;
+    long long best = 1, best_cost = 0;
+    for (long long s = 1; s <= tiles && s <= kMaxSplits; ++s) {
+        const long long per = (tiles + s - 1) / s, waves = (blocks * s + resident - 1) / resident, cost = waves * (per + 3) + (s > 1 ? 2 : 0);
+        if (s == 1 || cost < best_cost) best = s, best_cost = cost;
+    }
+    return (int)best;
+}
+bool on_tensor_cores(const rkv_desc_t *d) { return rows_sm100_supported(d->dtype, d->head_dim, d->n_q_heads / d->n_kv_heads); }
+int splits_for(const rkv_desc_t *d, const RowsParams &p)
+{
+    const long long sms = sm_count();
+    if (!on_tensor_cores(d)) return rows_splits(p, p.group >= kSimtRows ? 1 : kSimtRows / p.group, 2 * sms);
+    const int tiles = rows_sm100_tiles(p);
+    return rows_splits(p, tiles * (kTile / p.group), tiles == 2 ? sms : 2 * sms);
+}
+cudaError_t launch_rows(const rkv_desc_t *d, const RowsParams &p, cudaStream_t s)
+{
+    return on_tensor_cores(d) ? launch_rows_sm100(p, s) : launch_rows_simt(p, d->dtype, s);
 }
 size_t part_bytes(const RowsParams &p) { return align_up((size_t)p.tokens.total * p.hq * p.slots * (p.d + 2) * sizeof(float), 256); }
 
@@ -93,7 +110,7 @@ int plan_window(const rkv_desc_t *d, int budget, int buffer, const rkv_tokens_t 
     p->causal = 1;
     p->window = window;
     p->sinks = sinks;
-    p->splits = p->slots = simt_splits(*p);
+    p->splits = p->slots = splits_for(d, *p);
     *bytes = p->slots > 1 ? part_bytes(*p) : 0;
     return RKV_OK;
 }
@@ -101,7 +118,7 @@ int plan_window(const rkv_desc_t *d, int budget, int buffer, const rkv_tokens_t 
 int check_prefix(const rkv_desc_t *d, const rkv_prefix_t *x)
 {
     if (!x || x->count < 1 || d->batch % x->count != 0 || x->rows < 1) return RKV_ERR_INVALID_ARG;
-    if (x->rows > RKV_MAX_ROWS) return RKV_ERR_UNSUPPORTED;
+    if (x->rows > RKV_MAX_ROWS || (!x->table && (long long)x->count * d->n_kv_heads * x->rows > 0x7fffffffll)) return RKV_ERR_UNSUPPORTED;
     if (x->table && (x->rows % kTile != 0 || x->pages < 1 || x->pages > (1ll << 23) || (reinterpret_cast<uintptr_t>(x->table) & 3u)))
         return RKV_ERR_INVALID_ARG;
     return RKV_OK;
@@ -121,8 +138,8 @@ int plan_prefix(const rkv_desc_t *d, int budget, int buffer, const rkv_prefix_t 
     shared->tokens = TokenMap{nullptr, x->count, d->batch, d->batch / x->count};
     fill_rows(d, budget + buffer, own);
     own->tokens = TokenMap{nullptr, d->batch, d->batch, 1};
-    shared->splits = simt_splits(*shared);
-    own->splits = simt_splits(*own);
+    shared->splits = splits_for(d, *shared);
+    own->splits = splits_for(d, *own);
     own->slot = shared->splits;
     shared->slots = own->slots = shared->splits + own->splits;
     *bytes = part_bytes(*own);
@@ -208,7 +225,7 @@ int rkv_window_attention(const rkv_desc_t *d, const void *k_cache, const void *v
     p.out = out;
     p.part = bytes ? static_cast<float *>(d->workspace) : nullptr;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    cudaError_t e = launch_rows_simt(p, d->dtype, s);
+    cudaError_t e = launch_rows(d, p, s);
     if (e == cudaSuccess && p.part) e = launch_rows_merge(p, d->dtype, s);
     return e == cudaSuccess ? RKV_OK : cuda_fail(e, "window attention launch");
 }
@@ -241,8 +258,8 @@ int rkv_prefix_attention(const rkv_desc_t *d, const void *k_cache, const void *v
         p->part = static_cast<float *>(d->workspace);
     }
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    cudaError_t e = launch_rows_simt(shared, d->dtype, s);
-    if (e == cudaSuccess) e = launch_rows_simt(own, d->dtype, s);
+    cudaError_t e = launch_rows(d, shared, s);
+    if (e == cudaSuccess) e = launch_rows(d, own, s);
     if (e == cudaSuccess) e = launch_rows_merge(own, d->dtype, s);
     return e == cudaSuccess ? RKV_OK : cuda_fail(e, "prefix attention launch");
 }

@@ -1,0 +1,420 @@
+// Attention of many query rows over a cache on the tensor cores (see RowsParams): bf16 products, fp32 accumulation and softmax.
+//
+//   S = Q K^T   [128 rows x 128 keys], Q and K tiles in shared memory, accumulator in tensor memory
+//   P = 2^(S c - m)   by four warps, a thread per row; rounded to bf16 and written back over S in tensor memory
+//   O += P V    P from tensor memory, V as TMA leaves it (keys along K, so the transposed form of the operand), O in tensor memory
+//
+// A block takes kTiles (one or two) row tiles of one (problem, KV head); a row tile holds 128 / G whole tokens with their G heads.  K and V
+// tiles come through one ring, K_0 V_0 K_1 V_1 ..; with two row tiles each serves both, and while four warps turn one tile's scores
+// into weights the tensor cores work for the other tile.
+//
+// The maximum that the weights refer to moves only when a row's scores outgrow it by 2^8: until then weights up to 2^8 are as exact as
+// others in bf16, and O and the sum need no correction.  O's correction happens behind the barrier of the next scores, which the tensor
+// cores reach after all products before them.
+//
+// Rows that nobody of the block sees may hold anything: their scores are masked, their V rows cleared in shared memory by the
+// producer warp before the tile is handed on (0 x NaN).  Only the border tiles have such rows.
+//
+// Every wait is bounded; on expiry the block records RKV_ERR_TIMEOUT and leaves through the common exit.  No TMA multicast.
+#include "rkv_sm100.cuh"
+#include "rkv_tokens.cuh"
+
+namespace rkv {
+
+namespace {
+
+using namespace sm100;
+
+template <int kDim, int kTiles>
+struct RowsShape {
+    static constexpr int kHalves = kDim / 64;
+    static constexpr int kBox = kTile * 64 * 2;                          // 128 rows x 64 columns
+    static constexpr int kTileBytes = kHalves * kBox;
+    static constexpr int kStages = kTiles == 2 ? (kDim == 128 ? 5 : 8) : (kDim == 128 ? 2 : 4);
+    static constexpr int kOffRing = kTiles * kTileBytes;
+    static constexpr int kOffBars = kOffRing + kStages * kTileBytes;
+    // barriers: full[stages], empty[stages], queries, border tile landed, scores[tiles], weights[tiles], output
+    static constexpr int kFull = 0, kEmpty = kFull + kStages, kQ = kEmpty + kStages, kBorder = kQ + 1, kScores = kBorder + 1,
+                         kWeights = kScores + kTiles, kOut = kWeights + kTiles, kBars = kOut + 1;
+    static constexpr int kOffMisc = kOffBars + kBars * 8;
+    static constexpr int kSmem = kOffMisc + 16 + 1024;
+    static constexpr int kThreads = kTiles * 128 + 64;
+    static constexpr uint32_t kCols = kTiles == 2 ? 512 : 256;
+    __host__ __device__ static constexpr int kScoreCol(int i) { return i * 128; }
+    __host__ __device__ static constexpr int kOutCol(int i) { return kTiles * 128 + i * kDim; }
+    static_assert(kTiles * (128 + kDim) <= (int)kCols, "tensor memory");
+    static_assert(kSmem <= (kTiles == 2 ? 227 : 113) * 1024, "shared memory");
+};
+
+constexpr float kSlack = 8.f;              // the weights' reference may fall behind the maximum by 2^8
+
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
+        "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]),
+        "r"(r[30]), "r"(r[31])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// D[128 x N] += A[128 x 16, tensor memory] . B[16 x N, shared memory]
+__device__ __forceinline__ void umma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accum)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accum)
+        : "memory");
+}
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar)
+        : "memory");
+}
+// 2^x to about 2^-22; results below 2^-126 are 0
+__device__ __forceinline__ float exp2_approx(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
+{
+    const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&b);
+}
+
+template <int kDim, int kTiles>
+__global__ void __launch_bounds__(RowsShape<kDim, kTiles>::kThreads, kTiles == 2 ? 1 : 2)
+rows_tc_kernel(RowsParams p, int tokens_per_tile, int blocks_per_problem, const __grid_constant__ CUtensorMap map_k,
+               const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_q)
+{
+    using S = RowsShape<kDim, kTiles>;
+    extern __shared__ uint8_t rows_tc_raw[];
+    uint8_t *smem = align_smem(rows_tc_raw);
+    const uint32_t sbase = smem_u32(smem);
+    uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(smem + S::kOffMisc);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + S::kOffMisc + 4);
+    auto bar = [&](int i) { return sbase + S::kOffBars + 8 * i; };
+    const ErrSink sink{p.status, nullptr, p.wait_cycles};
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    constexpr int kProducer = kTiles * 4, kIssuer = kProducer + 1;
+
+    pdl_wait();
+    // ---- the block's rows.  Without a window the last tokens see the most keys: they come first, of all problems
+    int x = blockIdx.x;
+    const int split = x % p.splits;
+    x /= p.splits;
+    const int pairs = p.hkv * p.tokens.count;
+    const int piece = p.window > 0 ? x % blocks_per_problem : blocks_per_problem - 1 - x / pairs;
+    const int pair = p.window > 0 ? x / blocks_per_problem : x % pairs;
+    const int h = pair % p.hkv, b = pair / p.hkv;
+    int first;
+    const int n = token_span(p.tokens, b, &first);
+    int len = p.lens[b];
+    if (n < 0 || len < 0 || len > p.cap || (p.causal && len < n)) {
+        if (threadIdx.x == 0) report(p.status, RKV_ERR_INVALID_ARG);
+        len = 0;
+    }
+    const int t0 = piece * kTiles * tokens_per_tile;                     // first token of the block
+    if (n <= 0 || t0 >= n) return;
+    const int t1 = min(n, t0 + kTiles * tokens_per_tile) - 1;            // its last
+    KeyTiles keys = key_tiles(p.causal, p.window, p.sinks, len, n, t0, t1);
+    if (len == 0) keys.count = 0;
+    const int per = (keys.count + p.splits - 1) / p.splits, i0 = split * per, T = max(0, min(keys.count, i0 + per) - i0);
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S::kStages; ++s) {
+            mbar_init(bar(S::kFull + s), 1);
+            mbar_init(bar(S::kEmpty + s), 1);
+        }
+        mbar_init(bar(S::kQ), 1);
+        mbar_init(bar(S::kBorder), 1);
+        for (int i = 0; i < kTiles; ++i) {
+            mbar_init(bar(S::kScores + i), 1);
+            mbar_init(bar(S::kWeights + i), 128);
+        }
+        mbar_init(bar(S::kOut), 1);
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == kIssuer) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                     ::"r"(smem_u32(tmem_holder)), "r"(S::kCols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_holder;
+    // Only now may a later kernel's blocks come in: one that took tensor memory and waited for this kernel's end, while a block of this
+    // kernel waited for tensor memory, would wait for good.
+    pdl_trigger();
+
+    if (warp == kProducer) {
+        // ------------------------------------------------------------------ TMA producer
+        const int head = b * p.hkv + h;
+        if (lane == 0 && T > 0) {
+            mbar_expect_tx(bar(S::kQ), kTiles * S::kHalves * 128 * tokens_per_tile * p.group);
+            for (int i = 0; i < kTiles; ++i)
+                for (int half = 0; half < S::kHalves; ++half)
+                    tma_load_3d(sbase + i * S::kTileBytes + half * S::kBox, &map_q, 64 * half, h * p.group, first + t0 + i * tokens_per_tile,
+                                bar(S::kQ));
+        }
+        int borders = 0;
+        bool ok = true;
+        for (int i = 0; i < 2 * T && ok; ++i) {
+            const int t = keys.tile(i0 + (i >> 1)), s = i % S::kStages, j0 = t * kTile;
+            const bool value = i & 1;
+            // rows that nobody sees: at or behind hi, or between the first ones and lo
+            const bool border = value && (j0 + kTile > keys.hi || (j0 < keys.lo && j0 + kTile > keys.sinks));
+            const long long start = rows_tile_start(p, head, t);
+            if (start < 0 && lane == 0) report(p.status, RKV_ERR_INVALID_ARG);
+            const int y = start < 0 ? -kTile : (int)start;               // (beyond the tensor: zeros)
+            ok = mbar_wait(bar(S::kEmpty + s), ((i / S::kStages) & 1) ^ 1, abort_flag, sink);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            const uint32_t dst = sbase + S::kOffRing + s * S::kTileBytes, full = border ? bar(S::kBorder) : bar(S::kFull + s);
+            if (lane == 0) {
+                mbar_expect_tx(full, S::kTileBytes);
+                for (int half = 0; half < S::kHalves; ++half) tma_load_2d(dst + half * S::kBox, value ? &map_v : &map_k, 64 * half, y, full);
+            }
+            if (border) {
+                ok = mbar_wait(full, borders++ & 1, abort_flag, sink);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                uint8_t *tile = smem + S::kOffRing + s * S::kTileBytes;
+                for (int r = 0; r < kTile; r += 4) {                     // 8 lanes to a row of a box
+                    const int row = r + (lane >> 3);
+                    if (!keys.wanted(j0 + row))
+                        for (int half = 0; half < S::kHalves; ++half)
+                            *reinterpret_cast<uint4 *>(tile + half * S::kBox + row * 128 + (lane & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(S::kFull + s));
+            }
+        }
+        __syncwarp();
+    } else if (warp == kIssuer) {
+        // ------------------------------------------------------------------ MMA issuer
+        if (lane == 0 && T > 0) {
+            const uint32_t idesc_s = instr_desc(kTile, kTile), idesc_o = instr_desc(kTile, kDim) | (1u << 16);      // V: keys along K
+            auto stage_of = [&](int i) { return sbase + S::kOffRing + (i % S::kStages) * S::kTileBytes; };
+            auto wait_full = [&](int i) { return mbar_wait(bar(S::kFull + i % S::kStages), (i / S::kStages) & 1, abort_flag, sink); };
+            auto scores = [&](int r, int j) {
+                if (kDim == 128) umma_tile_k128(tmem + S::kScoreCol(r), sbase + r * S::kTileBytes, stage_of(2 * j), idesc_s);
+                else umma_tile_k64(tmem + S::kScoreCol(r), sbase + r * S::kTileBytes, stage_of(2 * j), idesc_s);
+                umma_commit(bar(S::kScores + r));
+            };
+            auto values = [&](int r, int j) {
+                const uint32_t v = stage_of(2 * j + 1);
+#pragma unroll
+                for (int ks = 0; ks < kTile / 16; ++ks) {
+                    const uint32_t addr = v + ks * 2048;                 // 16 keys further
+                    const uint64_t db = (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(S::kBox >> 4) << 16) | ((uint64_t)(1024u >> 4) << 32) |
+                                        ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+                    umma_ts(tmem + S::kOutCol(r), tmem + S::kScoreCol(r) + 8 * ks, db, idesc_o, (j > 0 || ks > 0) ? 1u : 0u);
+                }
+            };
+            bool ok = mbar_wait(bar(S::kQ), 0, abort_flag, sink) && wait_full(0);
+            if (ok) {
+                tc_fence_after();
+                for (int r = 0; r < kTiles; ++r) scores(r, 0);
+                umma_commit(bar(S::kEmpty));
+            }
+            for (int j = 0; j < T && ok; ++j) {
+                for (int r = 0; r < kTiles && ok; ++r) {
+                    ok = (r > 0 || wait_full(2 * j + 1)) && mbar_wait(bar(S::kWeights + r), j & 1, abort_flag, sink);
+                    if (!ok) break;
+                    tc_fence_after();
+                    values(r, j);
+                    if (r == kTiles - 1) umma_commit(bar(S::kEmpty + (2 * j + 1) % S::kStages));
+                    if (j + 1 == T) continue;
+                    ok = r > 0 || wait_full(2 * j + 2);
+                    if (!ok) break;
+                    tc_fence_after();
+                    scores(r, j + 1);
+                    if (r == kTiles - 1) umma_commit(bar(S::kEmpty + (2 * j + 2) % S::kStages));
+                }
+            }
+            if (ok) umma_commit(bar(S::kOut));
+        }
+        __syncwarp();
+    } else {
+        // ------------------------------------------------------------------ softmax, a thread per row
+        const int r = warp >> 2, row = threadIdx.x & 127;                // row tile, row (= lane of tensor memory)
+        const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        const uint32_t s_col = lanes + S::kScoreCol(r), o_col = lanes + S::kOutCol(r);
+        const int tt0 = t0 + r * tokens_per_tile, tt1 = min(t1, tt0 + tokens_per_tile - 1);
+        const int t = tt0 + row / p.group, g = row % p.group;
+        const bool mine = row < tokens_per_tile * p.group && t <= t1;    // else: nobody's row, computed and dropped
+        // the cached rows that this row sees, and what all rows of the tile see
+        const int at = len - n + t, last = p.causal ? at : len - 1, from = p.causal && p.window > 0 ? at + 1 - p.window : 0;
+        const int last_all = p.causal ? len - n + tt0 : len - 1, from_all = p.causal && p.window > 0 ? len - n + tt1 + 1 - p.window : 0;
+        const float c2 = 1.4426950408889634f * rsqrtf((float)kDim);
+        float m = -INFINITY, l = 0.f;                                    // reference of the weights (raw scores), sum of weights
+        bool ok = true;
+        for (int j = 0; j < T; ++j) {
+            ok = __all_sync(0xffffffffu, mbar_wait(bar(S::kScores + r), j & 1, abort_flag, sink));
+            if (!ok) break;
+            tc_fence_after();
+            uint32_t s[4][32];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) tmem_ld32(s_col + 32 * c, s[c]);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) tmem_wait32(s[c]);
+            const int j0 = keys.tile(i0 + j) * kTile;
+            if (!(j0 + kTile - 1 <= last_all && (j0 >= from_all || j0 + kTile <= p.sinks))) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) {
+                        const int key = j0 + 32 * c + e;
+                        if (!(key <= last && (key >= from || key < p.sinks))) s[c][e] = 0xFF800000u;       // -inf
+                    }
+            }
+            float top[4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                top[c] = fmaxf(__uint_as_float(s[c][0]), __uint_as_float(s[c][1]));
+#pragma unroll
+                for (int e = 2; e < 32; e += 2) top[c] = fmaxf(top[c], fmaxf(__uint_as_float(s[c][e]), __uint_as_float(s[c][e + 1])));
+            }
+            const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+            const bool outgrown = (most - m) * c2 > kSlack || (m == -INFINITY && most > -INFINITY);
+            if (__any_sync(0xffffffffu, outgrown)) {
+                const float next = outgrown ? most : m, shrink = outgrown ? exp2f((m - next) * c2) : 1.f;
+                m = next;
+                l *= shrink;
+                if (j > 0) {
+                    // all products up to these scores are through: O is this warp's to change
+#pragma unroll 1
+                    for (int c = 0; c < kDim; c += 32) {
+                        uint32_t o[32];
+                        tmem_ld32(o_col + c, o);
+                        tmem_wait32(o);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * shrink);
+                        tmem_st32(o_col + c, o);
+                    }
+                }
+            }
+            const float base = m == -INFINITY ? 0.f : m * c2;
+            float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                uint32_t w[32];
+#pragma unroll
+                for (int e = 0; e < 32; ++e) {
+                    const float a = exp2_approx(fmaf(__uint_as_float(s[2 * half + (e >> 4)][(2 * e) & 31]), c2, -base));
+                    const float y = exp2_approx(fmaf(__uint_as_float(s[2 * half + (e >> 4)][(2 * e + 1) & 31]), c2, -base));
+                    sum[e & 1] += a;
+                    sum[2 + (e & 1)] += y;
+                    w[e] = pack_bf16(a, y);
+                }
+                tmem_st32(s_col + 32 * half, w);
+            }
+            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            tmem_st_wait();
+            tc_fence_before();
+            mbar_arrive(bar(S::kWeights + r));
+        }
+        if (ok && T > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar(S::kOut), 0, abort_flag, sink));
+        tc_fence_after();
+        const int qh = h * p.group + g;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        float *part = p.part ? p.part + (((size_t)(first + t) * p.hq + qh) * p.slots + p.slot + split) * (kDim + 2) : nullptr;
+        __nv_bfloat16 *out = p.part ? nullptr : static_cast<__nv_bfloat16 *>(p.out) + (first + t) * p.out_stride + (size_t)qh * kDim;
+#pragma unroll 1
+        for (int c = 0; c < kDim; c += 32) {
+            uint32_t o[32];
+            if (T > 0 && ok) {
+                tmem_ld32(o_col + c, o);
+                tmem_wait32(o);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 32; ++e) o[e] = 0u;
+            }
+            if (!mine) continue;
+            if (part) {
+#pragma unroll
+                for (int e = 0; e < 32; e += 2) *reinterpret_cast<uint2 *>(part + c + e) = make_uint2(o[e], o[e + 1]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 32; e += 8) {
+                    uint4 v;
+                    v.x = pack_bf16(__uint_as_float(o[e]) * inv, __uint_as_float(o[e + 1]) * inv);
+                    v.y = pack_bf16(__uint_as_float(o[e + 2]) * inv, __uint_as_float(o[e + 3]) * inv);
+                    v.z = pack_bf16(__uint_as_float(o[e + 4]) * inv, __uint_as_float(o[e + 5]) * inv);
+                    v.w = pack_bf16(__uint_as_float(o[e + 6]) * inv, __uint_as_float(o[e + 7]) * inv);
+                    *reinterpret_cast<uint4 *>(out + c + e) = v;
+                }
+            }
+        }
+        if (mine && part) *reinterpret_cast<float2 *>(part + kDim) = make_float2(ok && T > 0 ? m * c2 : -INFINITY, ok ? l : 0.f);
+    }
+
+    // ---------------------------------------------------------------------- common exit
+    tc_fence_before();
+    __syncthreads();
+    if (warp == kIssuer) {
+        if (*abort_flag) __nanosleep(200000);      // error path only: let copies and products in flight land
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::kCols) : "memory");
+    }
+}
+
+// The queries as [token][head][dim]: a box is a row tile's whole tokens with the group's heads, 64 dimensions at a time.
+bool make_map_queries(CUtensorMap *map, const RowsParams &p, int tokens_per_tile)
+{
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[3] = {(cuuint64_t)p.d, (cuuint64_t)p.hq, (cuuint64_t)p.tokens.total};
+    const cuuint64_t strides[2] = {(cuuint64_t)p.d * 2, (cuuint64_t)p.q_stride * 2};
+    const cuuint32_t box[3] = {64u, (cuuint32_t)p.group, (cuuint32_t)tokens_per_tile}, estr[3] = {1u, 1u, 1u};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(p.q), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int kDim, int kTiles>
+cudaError_t launch_tc_for(const RowsParams &p, cudaStream_t s)
+{
+    using S = RowsShape<kDim, kTiles>;
+    static PerDevice done;
+    int dev = 0, sms = 0;
+    cudaError_t e = device_sms(&dev, &sms);
+    if (e != cudaSuccess) return e;
+    if ((e = allow_smem_once(done, dev, rows_tc_kernel<kDim, kTiles>, S::kSmem)) != cudaSuccess) return e;
+    const int tokens = kTile / p.group;
+    const long long per_problem = ((long long)p.tokens.longest + kTiles * tokens - 1) / (kTiles * tokens);
+    const long long blocks = per_problem * p.hkv * p.tokens.count * p.splits;
+    if (blocks > 0x7fffffffll) return cudaErrorInvalidValue;
+    const uint64_t rows = p.block_table ? (uint64_t)p.pool_pages * kTile : (uint64_t)p.tokens.count * p.hkv * p.cap;
+    CUtensorMap mk, mv, mq;
+    if (!make_map_rows(&mk, p.k, rows, kDim, kTile) || !make_map_rows(&mv, p.v, rows, kDim, kTile) || !make_map_queries(&mq, p, tokens))
+        return cudaErrorInvalidValue;
+    return launch_early(rows_tc_kernel<kDim, kTiles>, (unsigned)blocks, S::kThreads, S::kSmem, s, 1, p, tokens, (int)per_problem, mk, mv, mq);
+}
+
+}  // namespace
+
+bool rows_sm100_supported(int dtype, int d, int group) { return dtype == RKV_BF16 && (d == 64 || d == 128) && group <= kTile; }
+
+// Two row tiles to a block where a problem has more than one.
+int rows_sm100_tiles(const RowsParams &p) { return p.tokens.longest > kTile / p.group ? 2 : 1; }
+
+cudaError_t launch_rows_sm100(const RowsParams &p, cudaStream_t s)
+{
+    if (rows_sm100_tiles(p) == 2) return p.d == 128 ? launch_tc_for<128, 2>(p, s) : launch_tc_for<64, 2>(p, s);
+    return p.d == 128 ? launch_tc_for<128, 1>(p, s) : launch_tc_for<64, 1>(p, s);
+}
+
+}  // namespace rkv

@@ -87,6 +87,9 @@ __device__ __forceinline__ long long rows_tile_start(const RowsParams &p, int he
     return page < 0 || page >= p.pool_pages ? -1 : (long long)page * kTile;
 }
 cudaError_t launch_rows_simt(const RowsParams &p, int dtype, cudaStream_t s);
+bool rows_sm100_supported(int dtype, int d, int group);
+int rows_sm100_tiles(const RowsParams &p);                  // row tiles of a block
+cudaError_t launch_rows_sm100(const RowsParams &p, cudaStream_t s);
 cudaError_t launch_rows_merge(const RowsParams &p, int dtype, cudaStream_t s);
 
 }  // namespace rkv
