@@ -49,11 +49,18 @@ int sm_count()
 // Splits of the blocks' key tiles.  `rows` query rows to a block, `resident` blocks on the GPU at a time: the shortest run, counted in
 // waves of blocks times the tiles of each and three more for its start and end; two more for the merge kernel.
 constexpr int kSimtRows = 64, kMaxSplits = 64;
+// key tiles that so many tokens in a row see at most
+long long tiles_seen(const RowsParams &p, int tokens)
+{
+    const long long all = (p.cap + kTile - 1) / kTile;
+    if (!p.causal || p.window == 0) return all;
+    const long long tiles = ((long long)p.window + tokens) / kTile + 2 + ((long long)p.sinks + kTile - 1) / kTile;
+    return tiles < all ? tiles : all;
+}
 int rows_splits(const RowsParams &p, int tokens_per_block, long long resident)
 {
     const long long blocks = ((long long)p.tokens.longest + tokens_per_block - 1) / tokens_per_block * p.hkv * p.tokens.count;
-    const long long seen = p.causal && p.window > 0 ? (long long)p.window + tokens_per_block : p.cap;
-    const long long tiles = seen < p.cap ? seen / kTile + 2 + (p.sinks < p.cap ? (p.sinks + kTile - 1) / kTile : 0) : (p.cap + kTile - 1) / kTile;
+    const long long tiles = tiles_seen(p, tokens_per_block);
     long long best = 1, best_cost = 0;
     for (long long s = 1; s <= tiles && s <= kMaxSplits; ++s) {
         const long long per = (tiles + s - 1) / s, waves = (blocks * s + resident - 1) / resident, cost = waves * (per + 3) + (s > 1 ? 2 : 0);
@@ -97,11 +104,20 @@ void fill_rows(const rkv_desc_t *d, int cap, RowsParams *p)
     p->splits = p->slots = 1;
 }
 
-int plan_window(const rkv_desc_t *d, int budget, int buffer, const rkv_tokens_t *tokens, int window, int sinks, RowsParams *p, size_t *bytes)
+// A call's kernels: the rows' kernel, or for single tokens the decode attention's.
+struct Plan {
+    RowsParams rows;
+    bool single, separate;       // separate: its splits are blocks of their own
+    size_t bytes;
+};
+bool back_to_back(const rkv_desc_t *d, int64_t stride) { return stride == 0 || stride == (int64_t)d->n_q_heads * d->head_dim; }
+
+int plan_window(const rkv_desc_t *d, int budget, int buffer, const rkv_tokens_t *tokens, int window, int sinks, Plan *x)
 {
     int rc = check_cache(d, budget, buffer);
     if (rc != RKV_OK) return rc;
-    *p = RowsParams{};
+    *x = Plan{};
+    RowsParams *p = &x->rows;
     if ((rc = check_tokens(d, tokens, &p->tokens)) != RKV_OK) return rc;
     if (window < 0 || sinks < 0) return RKV_ERR_INVALID_ARG;
     const long long rows = (long long)tokens->longest * (d->n_q_heads / d->n_kv_heads);
@@ -110,8 +126,17 @@ int plan_window(const rkv_desc_t *d, int budget, int buffer, const rkv_tokens_t 
     p->causal = 1;
     p->window = window;
     p->sinks = sinks;
-    p->splits = p->slots = splits_for(d, *p);
-    *bytes = p->slots > 1 ? part_bytes(*p) : 0;
+    const long long tiles = tiles_seen(*p, 1);
+    x->single = !tokens->offsets && tokens->longest == 1 && back_to_back(d, tokens->q_stride) && back_to_back(d, tokens->out_stride) &&
+                attend_more_supported(d->dtype, d->head_dim, p->group, tiles);
+    if (x->single) {
+        attend_more_plan(p, d->dtype, tiles, sm_count(), &x->separate);
+        p->slots = x->separate ? p->splits : 0;
+        x->bytes = x->separate ? part_bytes(*p) : 0;
+    } else {
+        p->splits = p->slots = splits_for(d, *p);
+        x->bytes = p->slots > 1 ? part_bytes(*p) : 0;
+    }
     return RKV_OK;
 }
 
@@ -124,25 +149,29 @@ int check_prefix(const rkv_desc_t *d, const rkv_prefix_t *x)
     return RKV_OK;
 }
 
-// shared: the prefixes' rows; own: the sequences'.  Both leave partial results, side by side in a row's slots.
-int plan_prefix(const rkv_desc_t *d, int budget, int buffer, const rkv_prefix_t *x, RowsParams *shared, RowsParams *own, size_t *bytes)
+// shared: the prefixes' rows, whose partial results are a row's first slots; own: the sequences'.
+int plan_prefix(const rkv_desc_t *d, int budget, int buffer, const rkv_prefix_t *x, RowsParams *shared, Plan *own)
 {
     int rc = check_cache(d, budget, buffer);
     if (rc != RKV_OK || (rc = check_prefix(d, x)) != RKV_OK) return rc;
     if ((long long)d->batch * d->n_q_heads > (1ll << 28)) return RKV_ERR_UNSUPPORTED;
     *shared = RowsParams{};
-    *own = RowsParams{};
+    *own = Plan{};
+    RowsParams *p = &own->rows;
     fill_rows(d, x->rows, shared);
     shared->block_table = x->table;
     shared->pool_pages = x->pages;
     shared->tokens = TokenMap{nullptr, x->count, d->batch, d->batch / x->count};
-    fill_rows(d, budget + buffer, own);
-    own->tokens = TokenMap{nullptr, d->batch, d->batch, 1};
     shared->splits = splits_for(d, *shared);
-    own->splits = splits_for(d, *own);
-    own->slot = shared->splits;
-    shared->slots = own->slots = shared->splits + own->splits;
-    *bytes = part_bytes(*own);
+    fill_rows(d, budget + buffer, p);
+    p->tokens = TokenMap{nullptr, d->batch, d->batch, 1};
+    const long long tiles = tiles_seen(*p, 1);
+    own->single = attend_more_supported(d->dtype, d->head_dim, p->group, tiles);
+    if (own->single) attend_more_plan(p, d->dtype, tiles, sm_count(), &own->separate);
+    else p->splits = splits_for(d, *p);
+    p->slot = shared->splits;
+    shared->slots = p->slots = shared->splits + (own->single && !own->separate ? 0 : p->splits);
+    own->bytes = part_bytes(*p);
     return RKV_OK;
 }
 
@@ -197,61 +226,60 @@ int rkv_append_rotary(const rkv_desc_t *d, void *k_cache, void *v_cache, const v
 size_t rkv_window_workspace_bytes(const rkv_desc_t *d, int32_t budget, int32_t buffer, const rkv_tokens_t *tokens, int32_t window,
                                   int32_t sinks)
 {
-    RowsParams p;
-    size_t bytes = 0;
-    return plan_window(d, budget, buffer, tokens, window, sinks, &p, &bytes) == RKV_OK ? bytes : 0;
+    Plan x;
+    return plan_window(d, budget, buffer, tokens, window, sinks, &x) == RKV_OK ? x.bytes : 0;
 }
 
 int rkv_window_attention(const rkv_desc_t *d, const void *k_cache, const void *v_cache, const void *q, const int32_t *seq_lens, void *out,
                          int32_t budget, int32_t buffer, const rkv_tokens_t *tokens, int32_t window, int32_t sinks, void *stream)
 {
-    RowsParams p;
-    size_t bytes = 0;
-    int rc = plan_window(d, budget, buffer, tokens, window, sinks, &p, &bytes);
+    Plan x;
+    int rc = plan_window(d, budget, buffer, tokens, window, sinks, &x);
     if (rc != RKV_OK) return rc;
     if (!k_cache || !v_cache || !q || !seq_lens || !out) return RKV_ERR_INVALID_ARG;
     if (!aligned16(k_cache) || !aligned16(v_cache) || !aligned16(q) || !aligned16(out)) return RKV_ERR_INVALID_ARG;
     if (reinterpret_cast<uintptr_t>(seq_lens) & 3u) return RKV_ERR_INVALID_ARG;
+    RowsParams &p = x.rows;
     const size_t esz = d->dtype == RKV_F32 ? 4 : 2;
     p.q_stride = row_stride(tokens->q_stride, d->n_q_heads, d->head_dim, esz);
     p.out_stride = row_stride(tokens->out_stride, d->n_q_heads, d->head_dim, esz);
     if (!p.q_stride || !p.out_stride) return RKV_ERR_INVALID_ARG;
-    if ((rc = check_room(d, bytes)) != RKV_OK) return rc;
+    if ((rc = check_room(d, x.bytes)) != RKV_OK) return rc;
     if (tokens->total == 0) return RKV_OK;
     p.q = q;
     p.k = k_cache;
     p.v = v_cache;
     p.lens = seq_lens;
     p.out = out;
-    p.part = bytes ? static_cast<float *>(d->workspace) : nullptr;
+    p.part = x.bytes ? static_cast<float *>(d->workspace) : nullptr;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    cudaError_t e = launch_rows(d, p, s);
+    cudaError_t e = x.single ? launch_attend_more(p, d->dtype, tiles_seen(p, 1), x.separate, 0, false, s) : launch_rows(d, p, s);
     if (e == cudaSuccess && p.part) e = launch_rows_merge(p, d->dtype, s);
     return e == cudaSuccess ? RKV_OK : cuda_fail(e, "window attention launch");
 }
 
 size_t rkv_prefix_workspace_bytes(const rkv_desc_t *d, int32_t budget, int32_t buffer, const rkv_prefix_t *prefix)
 {
-    RowsParams shared, own;
-    size_t bytes = 0;
-    return plan_prefix(d, budget, buffer, prefix, &shared, &own, &bytes) == RKV_OK ? bytes : 0;
+    RowsParams shared;
+    Plan own;
+    return plan_prefix(d, budget, buffer, prefix, &shared, &own) == RKV_OK ? own.bytes : 0;
 }
 
 int rkv_prefix_attention(const rkv_desc_t *d, const void *k_cache, const void *v_cache, const void *q_new, const int32_t *seq_lens, void *out,
                          int32_t budget, int32_t buffer, const rkv_prefix_t *prefix, void *stream)
 {
-    RowsParams shared, own;
-    size_t bytes = 0;
-    int rc = plan_prefix(d, budget, buffer, prefix, &shared, &own, &bytes);
+    RowsParams shared;
+    Plan own;
+    int rc = plan_prefix(d, budget, buffer, prefix, &shared, &own);
     if (rc != RKV_OK) return rc;
     if (!k_cache || !v_cache || !q_new || !seq_lens || !out || !prefix->k || !prefix->v || !prefix->lens) return RKV_ERR_INVALID_ARG;
     for (const void *x : {k_cache, v_cache, q_new, (const void *)out, prefix->k, prefix->v})
         if (!aligned16(x)) return RKV_ERR_INVALID_ARG;
     if ((reinterpret_cast<uintptr_t>(seq_lens) | reinterpret_cast<uintptr_t>(prefix->lens)) & 3u) return RKV_ERR_INVALID_ARG;
-    if ((rc = check_room(d, bytes)) != RKV_OK) return rc;
+    if ((rc = check_room(d, own.bytes)) != RKV_OK) return rc;
     shared.k = prefix->k, shared.v = prefix->v, shared.lens = prefix->lens;
-    own.k = k_cache, own.v = v_cache, own.lens = seq_lens;
-    for (RowsParams *p : {&shared, &own}) {
+    own.rows.k = k_cache, own.rows.v = v_cache, own.rows.lens = seq_lens;
+    for (RowsParams *p : {&shared, &own.rows}) {
         p->q = q_new;
         p->out = out;
         p->q_stride = p->out_stride = (long long)d->n_q_heads * d->head_dim;
@@ -259,8 +287,10 @@ int rkv_prefix_attention(const rkv_desc_t *d, const void *k_cache, const void *v
     }
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     cudaError_t e = launch_rows(d, shared, s);
-    if (e == cudaSuccess) e = launch_rows(d, own, s);
-    if (e == cudaSuccess) e = launch_rows_merge(own, d->dtype, s);
+    if (e == cudaSuccess)
+        e = own.single ? launch_attend_more(own.rows, d->dtype, tiles_seen(own.rows, 1), own.separate, shared.splits, true, s)
+                       : launch_rows(d, own.rows, s);
+    if (e == cudaSuccess && (!own.single || own.separate)) e = launch_rows_merge(own.rows, d->dtype, s);
     return e == cudaSuccess ? RKV_OK : cuda_fail(e, "prefix attention launch");
 }
 

@@ -1,0 +1,52 @@
+// Decode-step attention on the tensor cores (rkv_attend_tc.cuh) for single tokens that see part of their cache, or a shared prefix as well.
+#include "rkv_attend_tc.cuh"
+
+namespace rkv {
+
+namespace {
+
+int source_of(int dtype, int d) { return dtype == RKV_FP8_E4M3 ? 1 : d == 64 ? 2 : 0; }
+
+}  // namespace
+
+// `tiles`: key tiles that a token sees at most.
+bool attend_more_supported(int dtype, int d, int group, long long tiles)
+{
+    return dtype != RKV_F32 && attend_supported(group, dtype, d) && tiles <= (long long)kTcMaxSplits * 2 * kTcChunkTiles;
+}
+
+// Splits as for rkv_decode_attention; blocks of their own where those are the faster there (attend_tc_separate).
+void attend_more_plan(RowsParams *p, int dtype, long long tiles, int sms, bool *separate)
+{
+    const int heads = p->tokens.count * p->hkv;
+    p->splits = attend_tc_splits(heads, (int)tiles * kTile, sms);
+    *separate = p->splits > 1 && source_of(dtype, p->d) != 0 && (long long)heads * p->splits > 4ll * sms;
+}
+
+cudaError_t launch_attend_more(const RowsParams &r, int dtype, long long tiles, bool separate, int others, bool late, cudaStream_t s)
+{
+    AttendTcMore p = {};
+    p.seq_lens = r.lens;
+    p.out = static_cast<float *>(r.out);         // (of bf16)
+    p.separate = separate ? 1 : 0;
+    p.hkv = r.hkv;
+    p.hq = r.hq;
+    p.cap = r.cap;
+    p.splits = r.splits;
+    p.tiles_per_split = (int)((tiles + r.splits - 1) / r.splits);
+    p.status = r.status;
+    p.wait_cycles = r.wait_cycles;
+    p.block_table = r.block_table;
+    p.least = r.causal ? 1 : 0;
+    p.window = r.window;
+    p.sinks = r.sinks;
+    p.pool_pages = r.pool_pages;
+    p.slots = r.part;
+    p.slots_per_row = r.slots;
+    p.others = others;
+    p.late = late ? 1 : 0;
+    if (p.tiles_per_split > 2 * kTcChunkTiles) return cudaErrorInvalidValue;
+    return launch_tc_group(p, r.k, r.v, r.q, r.tokens.count, r.pool_pages, source_of(dtype, r.d), s);
+}
+
+}  // namespace rkv

@@ -41,8 +41,8 @@ __global__ void __launch_bounds__(kThreads) rows_simt_kernel(RowsParams p, int r
     static_assert(kRows == kKeys, "one strip of rows after the other");
     extern __shared__ float rows_smem[];
     float *sq = rows_smem, *sk = sq + kRows * kStride, *sv = sk + kKeys * kStride, *sp = sv + kKeys * kDim;
-    pdl_trigger();
     pdl_wait();
+    pdl_trigger();                                               // (in this order: see AttendTcMore::late)
     const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
     int x = blockIdx.x;
     const int split = x % p.splits;

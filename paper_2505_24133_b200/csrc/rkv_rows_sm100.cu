@@ -155,7 +155,7 @@ rows_tc_kernel(RowsParams p, int tokens_per_tile, int blocks_per_problem, const 
     tc_fence_after();
     const uint32_t tmem = *tmem_holder;
     // Only now may a later kernel's blocks come in: one that took tensor memory and waited for this kernel's end, while a block of this
-    // kernel waited for tensor memory, would wait for good.
+    // kernel waited for tensor memory, would wait for good.  (And only behind the wait above: see AttendTcMore::late.)
     pdl_trigger();
 
     if (warp == kProducer) {

@@ -90,6 +90,12 @@ cudaError_t launch_rows_simt(const RowsParams &p, int dtype, cudaStream_t s);
 bool rows_sm100_supported(int dtype, int d, int group);
 int rows_sm100_tiles(const RowsParams &p);                  // row tiles of a block
 cudaError_t launch_rows_sm100(const RowsParams &p, cudaStream_t s);
+// One token per problem by the decode attention's kernel (rkv_attend_tc.cuh): K and V at the rate that memory gives.  p.slots > 0: slots of
+// other kernels, and of the splits where they are blocks of their own (then the merge kernel follows); `late`: the kernel before this one
+// leaves those slots and lets this one in only when everything before itself is done.
+bool attend_more_supported(int dtype, int d, int group, long long tiles);
+void attend_more_plan(RowsParams *p, int dtype, long long tiles, int sms, bool *separate);
+cudaError_t launch_attend_more(const RowsParams &p, int dtype, long long tiles, bool separate, int others, bool late, cudaStream_t s);
 cudaError_t launch_rows_merge(const RowsParams &p, int dtype, cudaStream_t s);
 
 }  // namespace rkv
