@@ -1,16 +1,20 @@
 // Attention of many query rows over a cache on the tensor cores (see RowsParams): bf16 products, fp32 accumulation and softmax.
 //
 //   S = Q K^T   [128 rows x 128 keys], Q and K tiles in shared memory, accumulator in tensor memory
-//   P = 2^(S c - m)   by four warps, a thread per row; rounded to bf16 and written back over S in tensor memory
+//   P = 2^(S c - m)   by eight warps, two threads per row, 64 keys each; rounded to bf16 and written back over S in tensor memory
 //   O += P V    P from tensor memory, V as TMA leaves it (keys along K, so the transposed form of the operand), O in tensor memory
 //
-// A block takes kTiles (one or two) row tiles of one (problem, KV head); a row tile holds 128 / G whole tokens with their G heads.  K and V
-// tiles come through one ring, K_0 V_0 K_1 V_1 ..; with two row tiles each serves both, and while four warps turn one tile's scores
-// into weights the tensor cores work for the other tile.
+// A block takes kTiles (one or two) row tiles of one (problem, KV head); a row tile holds 128 / G whole tokens with their G heads.
+//
+// Two row tiles (one block to an SM): each K and V tile serves both.  The scores have one accumulator, which the row tiles take in turn, and the
+// weights columns of their own: as soon as a tile's threads have its scores in registers the tensor cores form the other tile's, so scores are
+// there before the threads that need them and nobody waits for a chain of product, weights, product, scores (with the weights over
+// the scores, and two accumulators, that chain took 4700 cycles for 128 keys where the products take 2048).  Order of the products:
+// S_0(j+1) after S_1(j) has been read, then O_1(j-1), S_1(j+1), O_0(j) .., tiles K_0 K_1 V_0 K_2 V_1 ..
+// One row tile (two blocks to an SM): weights over the scores, S(j), O(j), S(j+1) .., tiles K_0 V_0 K_1 V_1 ..; the blocks fill each other's gaps.
 //
 // The maximum that the weights refer to moves only when a row's scores outgrow it by 2^8: until then weights up to 2^8 are as exact as
-// others in bf16, and O and the sum need no correction.  O's correction happens behind the barrier of the next scores, which the tensor
-// cores reach after all products before them.
+// others in bf16, and O and the sum need no correction.
 //
 // Rows that nobody of the block sees may hold anything: their scores are masked, their V rows cleared in shared memory by the
 // producer warp before the tile is handed on (0 x NaN).  Only the border tiles have such rows.
@@ -30,34 +34,47 @@ struct RowsShape {
     static constexpr int kHalves = kDim / 64;
     static constexpr int kBox = kTile * 64 * 2;                          // 128 rows x 64 columns
     static constexpr int kTileBytes = kHalves * kBox;
-    static constexpr int kStages = kTiles == 2 ? (kDim == 128 ? 5 : 8) : (kDim == 128 ? 2 : 4);
+    static constexpr int kStages = kTiles == 2 ? (kDim == 128 ? 4 : 8) : (kDim == 128 ? 2 : 4);
     static constexpr int kOffRing = kTiles * kTileBytes;
     static constexpr int kOffBars = kOffRing + kStages * kTileBytes;
-    // barriers: full[stages], empty[stages], queries, border tile landed, scores[tiles], weights[tiles], output
+    // barriers: full[stages], empty[stages], queries, border tile landed, scores[tiles], weights[tiles], ..
     static constexpr int kFull = 0, kEmpty = kFull + kStages, kQ = kEmpty + kStages, kBorder = kQ + 1, kScores = kBorder + 1,
-                         kWeights = kScores + kTiles, kOut = kWeights + kTiles, kBars = kOut + 1;
+                         kWeights = kScores + kTiles, kOut = kWeights + kTiles,           // kOut[tiles]: a product with V is through
+                         kRead = kOut + kTiles, kBars = kRead + kTiles;                    // kRead[tiles]: scores in registers
     static constexpr int kOffMisc = kOffBars + kBars * 8;
-    static constexpr int kSmem = kOffMisc + 16 + 1024;
-    static constexpr int kThreads = kTiles * 128 + 64;
+    static constexpr int kOffMost = (kOffMisc + 16 + 15) / 16 * 16;      // [tiles][2 halves][128]: the rows' largest scores, later sums
+    static constexpr int kSmem = kOffMost + kTiles * 256 * 4 + 1024;
+    static constexpr int kThreads = kTiles * 256 + 64;
     static constexpr uint32_t kCols = kTiles == 2 ? 512 : 256;
-    __host__ __device__ static constexpr int kScoreCol(int i) { return i * 128; }
+    // tensor memory: scores, weights, outputs; one row tile: the weights of each half of the keys over its scores
+    __host__ __device__ static constexpr int kWeightCol(int i, int half) { return kTiles == 2 ? 128 + i * 64 + half * 32 : half * 64; }
     __host__ __device__ static constexpr int kOutCol(int i) { return kTiles * 128 + i * kDim; }
+    // the ring's i-th tile of 2 T: K or V, and of which keys; and the places of K_j and V_j
+    __device__ static __forceinline__ bool value_at(int i, int T) { return kTiles == 1 || T == 1 ? i & 1 : i == 2 * T - 1 || (i >= 2 && !(i & 1)); }
+    __device__ static __forceinline__ int index_at(int i, int T)
+    {
+        return kTiles == 1 || T == 1 ? i >> 1 : i == 2 * T - 1 ? T - 1 : i < 2 ? i : i & 1 ? (i + 1) >> 1 : (i - 2) >> 1;
+    }
+    __device__ static __forceinline__ int place_k(int j, int T) { return kTiles == 1 || T == 1 ? 2 * j : j == 0 ? 0 : 2 * j - 1; }
+    __device__ static __forceinline__ int place_v(int j, int T) { return kTiles == 1 || T == 1 ? 2 * j + 1 : j == T - 1 ? 2 * T - 1 : 2 * j + 2; }
     static_assert(kTiles * (128 + kDim) <= (int)kCols, "tensor memory");
     static_assert(kSmem <= (kTiles == 2 ? 227 : 113) * 1024, "shared memory");
 };
 
 constexpr float kSlack = 8.f;              // the weights' reference may fall behind the maximum by 2^8
 
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32])
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16])
 {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
         ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
-        "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]),
-        "r"(r[30]), "r"(r[31])
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -70,6 +87,13 @@ __device__ __forceinline__ void umma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64
         "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
         ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accum)
         : "memory");
+}
+// true for one lane of the warp
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t is;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(is));
+    return is != 0;
 }
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar)
 {
@@ -85,6 +109,29 @@ __device__ __forceinline__ float exp2_approx(float x)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// two fp32 at a time
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, c, d;\n\t"
+        "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+        "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, d;\n\t"
+        "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
+        "add.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+// bit e set: e <= last
+__device__ __forceinline__ uint32_t bits_to(int last) { return last < 0 ? 0u : last >= 31 ? 0xFFFFFFFFu : (2u << last) - 1u; }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
 {
     const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
@@ -105,7 +152,7 @@ rows_tc_kernel(RowsParams p, int tokens_per_tile, int blocks_per_problem, const 
     auto bar = [&](int i) { return sbase + S::kOffBars + 8 * i; };
     const ErrSink sink{p.status, nullptr, p.wait_cycles};
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    constexpr int kProducer = kTiles * 4, kIssuer = kProducer + 1;
+    constexpr int kProducer = kTiles * 8, kIssuer = kProducer + 1;
 
     pdl_wait();
     // ---- the block's rows.  Without a window the last tokens see the most keys: they come first, of all problems
@@ -139,9 +186,10 @@ rows_tc_kernel(RowsParams p, int tokens_per_tile, int blocks_per_problem, const 
         mbar_init(bar(S::kBorder), 1);
         for (int i = 0; i < kTiles; ++i) {
             mbar_init(bar(S::kScores + i), 1);
-            mbar_init(bar(S::kWeights + i), 128);
+            mbar_init(bar(S::kWeights + i), 256);
+            mbar_init(bar(S::kOut + i), 1);
+            mbar_init(bar(S::kRead + i), 256);
         }
-        mbar_init(bar(S::kOut), 1);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -171,8 +219,8 @@ rows_tc_kernel(RowsParams p, int tokens_per_tile, int blocks_per_problem, const 
         int borders = 0;
         bool ok = true;
         for (int i = 0; i < 2 * T && ok; ++i) {
-            const int t = keys.tile(i0 + (i >> 1)), s = i % S::kStages, j0 = t * kTile;
-            const bool value = i & 1;
+            const bool value = S::value_at(i, T);
+            const int t = keys.tile(i0 + S::index_at(i, T)), s = i % S::kStages, j0 = t * kTile;
             // rows that nobody sees: at or behind hi, or between the first ones and lo
             const bool border = value && (j0 + kTile > keys.hi || (j0 < keys.lo && j0 + kTile > keys.sinks));
             const long long start = rows_tile_start(p, head, t);
@@ -205,54 +253,81 @@ rows_tc_kernel(RowsParams p, int tokens_per_tile, int blocks_per_problem, const 
         __syncwarp();
     } else if (warp == kIssuer) {
         // ------------------------------------------------------------------ MMA issuer
-        if (lane == 0 && T > 0) {
+        // The whole warp goes through the loop and the waits, so that descriptors stay in uniform registers; one elected lane issues.  (With
+        // the loop in one lane's branch a product of 16 took 65 to 85 cycles to issue, twice what it takes to run.)
+        if (T > 0) {
+            const bool leader = elect_one();
             const uint32_t idesc_s = instr_desc(kTile, kTile), idesc_o = instr_desc(kTile, kDim) | (1u << 16);      // V: keys along K
-            auto stage_of = [&](int i) { return sbase + S::kOffRing + (i % S::kStages) * S::kTileBytes; };
-            auto wait_full = [&](int i) { return mbar_wait(bar(S::kFull + i % S::kStages), (i / S::kStages) & 1, abort_flag, sink); };
-            auto scores = [&](int r, int j) {
-                if (kDim == 128) umma_tile_k128(tmem + S::kScoreCol(r), sbase + r * S::kTileBytes, stage_of(2 * j), idesc_s);
-                else umma_tile_k64(tmem + S::kScoreCol(r), sbase + r * S::kTileBytes, stage_of(2 * j), idesc_s);
-                umma_commit(bar(S::kScores + r));
-            };
-            auto values = [&](int r, int j) {
-                const uint32_t v = stage_of(2 * j + 1);
+            const uint64_t q_desc = smem_desc(sbase), k_desc = smem_desc(sbase + S::kOffRing);
+            // V: 64 columns to a box, boxes kBox apart; 8 keys every 1024 bytes
+            const uint64_t v_desc = (uint64_t)(((sbase + S::kOffRing) & 0x3FFFFu) >> 4) | ((uint64_t)(S::kBox >> 4) << 16) |
+                                    ((uint64_t)(1024u >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+            constexpr uint32_t kStep = S::kTileBytes >> 4;               // from stage to stage, in a descriptor's units
+            auto scores = [&](int r, int j, bool free_stage) {
+                const int i = S::place_k(j, T);
+                const uint64_t dq = q_desc + (uint64_t)(r * kStep), dk = k_desc + (uint64_t)((i % S::kStages) * kStep);
+                if (leader) {
 #pragma unroll
-                for (int ks = 0; ks < kTile / 16; ++ks) {
-                    const uint32_t addr = v + ks * 2048;                 // 16 keys further
-                    const uint64_t db = (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(S::kBox >> 4) << 16) | ((uint64_t)(1024u >> 4) << 32) |
-                                        ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
-                    umma_ts(tmem + S::kOutCol(r), tmem + S::kScoreCol(r) + 8 * ks, db, idesc_o, (j > 0 || ks > 0) ? 1u : 0u);
+                    for (int ks = 0; ks < kDim / 16; ++ks) {
+                        const uint64_t off = (ks >> 2) * (S::kBox >> 4) + (ks & 3) * 2;      // 16 columns further
+                        umma(tmem, dq + off, dk + off, idesc_s, ks > 0 ? 1u : 0u);
+                    }
+                    umma_commit(bar(S::kScores + r));
+                    if (free_stage) umma_commit(bar(S::kEmpty + i % S::kStages));
                 }
             };
-            bool ok = mbar_wait(bar(S::kQ), 0, abort_flag, sink) && wait_full(0);
-            if (ok) {
-                tc_fence_after();
-                for (int r = 0; r < kTiles; ++r) scores(r, 0);
-                umma_commit(bar(S::kEmpty));
-            }
-            for (int j = 0; j < T && ok; ++j) {
-                for (int r = 0; r < kTiles && ok; ++r) {
-                    ok = (r > 0 || wait_full(2 * j + 1)) && mbar_wait(bar(S::kWeights + r), j & 1, abort_flag, sink);
-                    if (!ok) break;
+            auto values = [&](int r, int j, bool free_stage) {
+                const int i = S::place_v(j, T);
+                const uint64_t dv = v_desc + (uint64_t)((i % S::kStages) * kStep);
+                if (leader) {
+#pragma unroll
+                    for (int ks = 0; ks < kTile / 16; ++ks)              // 16 keys further
+                        umma_ts(tmem + S::kOutCol(r), tmem + S::kWeightCol(r, ks >> 2) + (ks & 3) * 8, dv + (uint64_t)(ks * 128), idesc_o,
+                                ks > 0 ? 1u : (uint32_t)(j > 0));
+                    umma_commit(bar(S::kOut + r));
+                    if (free_stage) umma_commit(bar(S::kEmpty + i % S::kStages));
+                }
+            };
+            auto full = [&](int i) { return mbar_wait(bar(S::kFull + i % S::kStages), (i / S::kStages) & 1, abort_flag, sink); };
+            auto weights = [&](int r, int j) { return mbar_wait(bar(S::kWeights + r), j & 1, abort_flag, sink); };
+            auto read = [&](int r, int j) { return mbar_wait(bar(S::kRead + r), j & 1, abort_flag, sink); };
+            bool ok = mbar_wait(bar(S::kQ), 0, abort_flag, sink) && full(0);
+            tc_fence_after();
+            if (ok) scores(0, 0, kTiles == 1);
+            if constexpr (kTiles == 1) {
+                for (int j = 0; j < T && ok; ++j) {
+                    if (!(ok = full(2 * j + 1) && weights(0, j))) break;
                     tc_fence_after();
-                    values(r, j);
-                    if (r == kTiles - 1) umma_commit(bar(S::kEmpty + (2 * j + 1) % S::kStages));
-                    if (j + 1 == T) continue;
-                    ok = r > 0 || wait_full(2 * j + 2);
-                    if (!ok) break;
+                    values(0, j, true);
+                    if (j + 1 == T) break;
+                    if (!(ok = full(2 * j + 2))) break;
+                    scores(0, j + 1, true);
+                }
+            } else {
+                // A wait costs some 100 cycles even where nothing is left to wait for: one between any two products, which the product before
+                // hides.  (That a tile's scores have been read says that its weights before them are there.)
+                for (int j = 0; j <= T && ok; ++j) {
+                    if (!(ok = j < T ? read(0, j) : weights(0, j - 1))) break;
                     tc_fence_after();
-                    scores(r, j + 1);
-                    if (r == kTiles - 1) umma_commit(bar(S::kEmpty + (2 * j + 2) % S::kStages));
+                    if (j < T) scores(1, j, true);
+                    if (j + 1 < T && !(ok = full(S::place_k(j + 1, T)))) break;
+                    if (j > 0) values(0, j - 1, false);
+                    if (!(ok = j < T ? read(1, j) : weights(1, j - 1))) break;
+                    tc_fence_after();
+                    if (j + 1 < T) scores(0, j + 1, false);
+                    if (j < T && !(ok = full(S::place_v(j, T)))) break;
+                    if (j > 0) values(1, j - 1, true);
                 }
             }
-            if (ok) umma_commit(bar(S::kOut));
         }
         __syncwarp();
     } else {
-        // ------------------------------------------------------------------ softmax, a thread per row
-        const int r = warp >> 2, row = threadIdx.x & 127;                // row tile, row (= lane of tensor memory)
+        // ------------------------------------------------------------------ softmax, two threads per row
+        const int r = warp >> 3, half = (warp >> 2) & 1, row = threadIdx.x & 127;        // row tile, keys 64 half .., row (= lane of tensor memory)
         const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-        const uint32_t s_col = lanes + S::kScoreCol(r), o_col = lanes + S::kOutCol(r);
+        const uint32_t s_col = lanes + 64 * half, w_col = lanes + S::kWeightCol(r, half), o_col = lanes + S::kOutCol(r) + half * (kDim / 2);
+        float *mosts = reinterpret_cast<float *>(smem + S::kOffMost) + r * 256;
+        auto pair_sync = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(1 + r * 4 + (warp & 3)) : "memory"); };       // the two warps of 32 rows
         const int tt0 = t0 + r * tokens_per_tile, tt1 = min(t1, tt0 + tokens_per_tile - 1);
         const int t = tt0 + row / p.group, g = row % p.group;
         const bool mine = row < tokens_per_tile * p.group && t <= t1;    // else: nobody's row, computed and dropped
@@ -260,81 +335,106 @@ rows_tc_kernel(RowsParams p, int tokens_per_tile, int blocks_per_problem, const 
         const int at = len - n + t, last = p.causal ? at : len - 1, from = p.causal && p.window > 0 ? at + 1 - p.window : 0;
         const int last_all = p.causal ? len - n + tt0 : len - 1, from_all = p.causal && p.window > 0 ? len - n + tt1 + 1 - p.window : 0;
         const float c2 = 1.4426950408889634f * rsqrtf((float)kDim);
-        float m = -INFINITY, l = 0.f;                                    // reference of the weights (raw scores), sum of weights
+        float m = -INFINITY, l = 0.f;                                    // reference of the weights (raw scores), sum of this thread's weights
         bool ok = true;
         for (int j = 0; j < T; ++j) {
-            ok = __all_sync(0xffffffffu, mbar_wait(bar(S::kScores + r), j & 1, abort_flag, sink));
-            if (!ok) break;
+            if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bar(S::kScores + r), j & 1, abort_flag, sink));
+            if (!ok) {                                                   // (every warp comes to every one of its pair's barriers)
+                pair_sync();
+                continue;
+            }
             tc_fence_after();
-            uint32_t s[4][32];
+            uint32_t s[2][32];
+            tmem_ld32(s_col, s[0]);
+            tmem_ld32(s_col + 32, s[1]);
+            tmem_wait32(s[0]);
+            tmem_wait32(s[1]);
+            if (kTiles == 2) {                                           // the accumulator is the other tile's
+                tc_fence_before();
+                mbar_arrive(bar(S::kRead + r));
+            }
+            const int j0 = keys.tile(i0 + j) * kTile + 64 * half;
+            if (!(j0 + 63 <= last_all && (j0 >= from_all || j0 + 64 <= p.sinks))) {
 #pragma unroll
-            for (int c = 0; c < 4; ++c) tmem_ld32(s_col + 32 * c, s[c]);
+                for (int c = 0; c < 2; ++c) {
+                    const int k0 = j0 + 32 * c;
+                    const uint32_t sees = bits_to(last - k0) & (~bits_to(from - 1 - k0) | bits_to(p.sinks - 1 - k0));
 #pragma unroll
-            for (int c = 0; c < 4; ++c) tmem_wait32(s[c]);
-            const int j0 = keys.tile(i0 + j) * kTile;
-            if (!(j0 + kTile - 1 <= last_all && (j0 >= from_all || j0 + kTile <= p.sinks))) {
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        const int key = j0 + 32 * c + e;
-                        if (!(key <= last && (key >= from || key < p.sinks))) s[c][e] = 0xFF800000u;       // -inf
-                    }
+                    for (int e = 0; e < 32; ++e)
+                        if (!(sees & (1u << e))) s[c][e] = 0xFF800000u;  // -inf
+                }
             }
             float top[4];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                top[c] = fmaxf(__uint_as_float(s[c][0]), __uint_as_float(s[c][1]));
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t *x = &s[i >> 1][(i & 1) * 16];
+                top[i] = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
 #pragma unroll
-                for (int e = 2; e < 32; e += 2) top[c] = fmaxf(top[c], fmaxf(__uint_as_float(s[c][e]), __uint_as_float(s[c][e + 1])));
+                for (int e = 2; e < 16; e += 2) top[i] = max3(top[i], __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
             }
-            const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+            float most = max3(fmaxf(top[0], top[1]), top[2], top[3]);
+            // (written again with the next scores, which come when all threads have handed in these weights)
+            mosts[half * 128 + row] = most;
+            pair_sync();
+            most = fmaxf(most, mosts[(half ^ 1) * 128 + row]);
             const bool outgrown = (most - m) * c2 > kSlack || (m == -INFINITY && most > -INFINITY);
             if (__any_sync(0xffffffffu, outgrown)) {
                 const float next = outgrown ? most : m, shrink = outgrown ? exp2f((m - next) * c2) : 1.f;
                 m = next;
                 l *= shrink;
                 if (j > 0) {
-                    // all products up to these scores are through: O is this warp's to change
+                    // all products so far are through (one row tile: they were before these scores): O is the row's threads' to change, a half each
+                    if (kTiles == 2) {
+                        ok = __all_sync(0xffffffffu, mbar_wait(bar(S::kOut + r), (j - 1) & 1, abort_flag, sink));
+                        tc_fence_after();
+                    }
 #pragma unroll 1
-                    for (int c = 0; c < kDim; c += 32) {
-                        uint32_t o[32];
-                        tmem_ld32(o_col + c, o);
-                        tmem_wait32(o);
+                    for (int c = 0; c < kDim / 2; c += 8) {              // (few registers at a time: the scores stay in theirs)
+                        uint32_t o[8];
+                        tmem_ld8(o_col + c, o);
+                        tmem_wait8(o);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * shrink);
-                        tmem_st32(o_col + c, o);
+                        for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * shrink);
+                        tmem_st8(o_col + c, o);
                     }
                 }
             }
-            const float base = m == -INFINITY ? 0.f : m * c2;
-            float sum[4] = {0.f, 0.f, 0.f, 0.f};
+            const float base = m == -INFINITY ? 0.f : -m * c2;
+            const float2 scale = make_float2(c2, c2), shift = make_float2(base, base);
+            float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+            uint32_t w[2][16];
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                uint32_t w[32];
+            for (int c = 0; c < 2; ++c)
 #pragma unroll
-                for (int e = 0; e < 32; ++e) {
-                    const float a = exp2_approx(fmaf(__uint_as_float(s[2 * half + (e >> 4)][(2 * e) & 31]), c2, -base));
-                    const float y = exp2_approx(fmaf(__uint_as_float(s[2 * half + (e >> 4)][(2 * e + 1) & 31]), c2, -base));
-                    sum[e & 1] += a;
-                    sum[2 + (e & 1)] += y;
-                    w[e] = pack_bf16(a, y);
+                for (int e = 0; e < 16; ++e) {
+                    float2 y = fma2(make_float2(__uint_as_float(s[c][2 * e]), __uint_as_float(s[c][2 * e + 1])), scale, shift);
+                    y = make_float2(exp2_approx(y.x), exp2_approx(y.y));
+                    sum[e & 1] = add2(sum[e & 1], y);
+                    w[c][e] = pack_bf16(y.x, y.y);
                 }
-                tmem_st32(s_col + 32 * half, w);
+            if (kTiles == 2 && j > 0 && ok) {                            // the weights before these have been read
+                ok = __all_sync(0xffffffffu, mbar_wait(bar(S::kOut + r), (j - 1) & 1, abort_flag, sink));
+                tc_fence_after();
             }
-            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            tmem_st16(w_col, w[0]);
+            tmem_st16(w_col + 16, w[1]);
+            sum[0] = add2(sum[0], sum[1]);
+            l += sum[0].x + sum[0].y;
             tmem_st_wait();
             tc_fence_before();
             mbar_arrive(bar(S::kWeights + r));
         }
-        if (ok && T > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar(S::kOut), 0, abort_flag, sink));
+        if (ok && T > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar(S::kOut + r), (T - 1) & 1, abort_flag, sink));
+        mosts[half * 128 + row] = l;
+        pair_sync();
+        l += mosts[(half ^ 1) * 128 + row];
         tc_fence_after();
-        const int qh = h * p.group + g;
+        const int qh = h * p.group + g, c0 = half * (kDim / 2);
         const float inv = l == 0.f ? 0.f : 1.f / l;
         float *part = p.part ? p.part + (((size_t)(first + t) * p.hq + qh) * p.slots + p.slot + split) * (kDim + 2) : nullptr;
         __nv_bfloat16 *out = p.part ? nullptr : static_cast<__nv_bfloat16 *>(p.out) + (first + t) * p.out_stride + (size_t)qh * kDim;
 #pragma unroll 1
-        for (int c = 0; c < kDim; c += 32) {
+        for (int c = 0; c < kDim / 2; c += 32) {
             uint32_t o[32];
             if (T > 0 && ok) {
                 tmem_ld32(o_col + c, o);
@@ -346,7 +446,7 @@ rows_tc_kernel(RowsParams p, int tokens_per_tile, int blocks_per_problem, const 
             if (!mine) continue;
             if (part) {
 #pragma unroll
-                for (int e = 0; e < 32; e += 2) *reinterpret_cast<uint2 *>(part + c + e) = make_uint2(o[e], o[e + 1]);
+                for (int e = 0; e < 32; e += 2) *reinterpret_cast<uint2 *>(part + c0 + c + e) = make_uint2(o[e], o[e + 1]);
             } else {
 #pragma unroll
                 for (int e = 0; e < 32; e += 8) {
@@ -355,11 +455,11 @@ rows_tc_kernel(RowsParams p, int tokens_per_tile, int blocks_per_problem, const 
                     v.y = pack_bf16(__uint_as_float(o[e + 2]) * inv, __uint_as_float(o[e + 3]) * inv);
                     v.z = pack_bf16(__uint_as_float(o[e + 4]) * inv, __uint_as_float(o[e + 5]) * inv);
                     v.w = pack_bf16(__uint_as_float(o[e + 6]) * inv, __uint_as_float(o[e + 7]) * inv);
-                    *reinterpret_cast<uint4 *>(out + c + e) = v;
+                    *reinterpret_cast<uint4 *>(out + c0 + c + e) = v;
                 }
             }
         }
-        if (mine && part) *reinterpret_cast<float2 *>(part + kDim) = make_float2(ok && T > 0 ? m * c2 : -INFINITY, ok ? l : 0.f);
+        if (mine && part && half == 0) *reinterpret_cast<float2 *>(part + kDim) = make_float2(ok && T > 0 ? m * c2 : -INFINITY, ok ? l : 0.f);
     }
 
     // ---------------------------------------------------------------------- common exit
