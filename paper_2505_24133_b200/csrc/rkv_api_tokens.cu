@@ -46,8 +46,6 @@ int sm_count()
     return device_sms(&dev, &sms) == cudaSuccess ? sms : 148;    // sizing only (no device here): the B200's count
 }
 
-// Splits of the blocks' key tiles.  `rows` query rows to a block, `resident` blocks on the GPU at a time: the shortest run, counted in
-// waves of blocks times the tiles of each and three more for its start and end; two more for the merge kernel.
 constexpr int kSimtRows = 64, kMaxSplits = 64;
 // key tiles that so many tokens in a row see at most
 long long tiles_seen(const RowsParams &p, int tokens)
@@ -57,13 +55,20 @@ long long tiles_seen(const RowsParams &p, int tokens)
     const long long tiles = ((long long)p.window + tokens) / kTile + 2 + ((long long)p.sinks + kTile - 1) / kTile;
     return tiles < all ? tiles : all;
 }
-int rows_splits(const RowsParams &p, int tokens_per_block, long long resident)
+// Splits of the key tiles: the shortest run, counted in key tiles of a block -- waves of blocks times the tiles of each and three more
+// for its start and end, and for the merge two and what it takes to write and read the shares at 4 TB/s (a key tile takes `tile_us`).
+// (Without that last term a chunk of 1000 tokens over 8000 rows was cut in four: 270 us, and 130 for the merge of 118 MB.)
+int rows_splits(const RowsParams &p, int tokens_per_block, long long resident, double tile_us)
 {
     const long long blocks = ((long long)p.tokens.longest + tokens_per_block - 1) / tokens_per_block * p.hkv * p.tokens.count;
     const long long tiles = tiles_seen(p, tokens_per_block);
-    long long best = 1, best_cost = 0;
+    const double share = (double)p.tokens.total * p.hq * (p.d + 2) * 4 * 2 / 4e6 / tile_us;
+    long long best = 1;
+    double best_cost = 0;
     for (long long s = 1; s <= tiles && s <= kMaxSplits; ++s) {
-        const long long per = (tiles + s - 1) / s, waves = (blocks * s + resident - 1) / resident, cost = waves * (per + 3) + (s > 1 ? 2 : 0);
+        const long long per = (tiles + s - 1) / s;
+        if (s > 1 && (tiles + per - 1) / per < s) continue;              // the last ones would have no tile
+        const double cost = (double)((blocks * s + resident - 1) / resident) * (per + 3) + (s > 1 ? 2 + s * share : 0);
         if (s == 1 || cost < best_cost) best = s, best_cost = cost;
     }
     return (int)best;
@@ -72,9 +77,9 @@ bool on_tensor_cores(const rkv_desc_t *d) { return rows_sm100_supported(d->dtype
 int splits_for(const rkv_desc_t *d, const RowsParams &p)
 {
     const long long sms = sm_count();
-    if (!on_tensor_cores(d)) return rows_splits(p, p.group >= kSimtRows ? 1 : kSimtRows / p.group, 2 * sms);
+    if (!on_tensor_cores(d)) return rows_splits(p, p.group >= kSimtRows ? 1 : kSimtRows / p.group, 2 * sms, 12.0);
     const int tiles = rows_sm100_tiles(p);
-    return rows_splits(p, tiles * (kTile / p.group), tiles == 2 ? sms : 2 * sms);
+    return rows_splits(p, tiles * (kTile / p.group), tiles == 2 ? sms : 2 * sms, 1.6);
 }
 cudaError_t launch_rows(const rkv_desc_t *d, const RowsParams &p, cudaStream_t s)
 {

@@ -16,8 +16,8 @@
 // The maximum that the weights refer to moves only when a row's scores outgrow it by 2^8: until then weights up to 2^8 are as exact as
 // others in bf16, and O and the sum need no correction.
 //
-// Rows that nobody of the block sees may hold anything: their scores are masked, their V rows cleared in shared memory by the
-// producer warp before the tile is handed on (0 x NaN).  Only the border tiles have such rows.
+// Rows that no token of the call sees may hold anything: their scores are masked, their V rows cleared in shared memory by the producer
+// warp before the tile is handed on (0 x NaN).  Only tiles at the borders of what the call sees have such rows.
 //
 // Every wait is bounded; on expiry the block records RKV_ERR_TIMEOUT and leaves through the common exit.  No TMA multicast.
 #include "rkv_sm100.cuh"
@@ -40,10 +40,12 @@ struct RowsShape {
     // barriers: full[stages], empty[stages], queries, border tile landed, scores[tiles], weights[tiles], ..
     static constexpr int kFull = 0, kEmpty = kFull + kStages, kQ = kEmpty + kStages, kBorder = kQ + 1, kScores = kBorder + 1,
                          kWeights = kScores + kTiles, kOut = kWeights + kTiles,           // kOut[tiles]: a product with V is through
-                         kRead = kOut + kTiles, kBars = kRead + kTiles;                    // kRead[tiles]: scores in registers
+                         kRead = kOut + kTiles,              // kRead[tiles]: scores in registers
+                         kFree = kRead + kTiles,             // kFree[tiles]: the output has left tensor memory
+                         kQFree = kFree + kTiles, kBars = kQFree + 1;                      // kQFree: the queries have been read
     static constexpr int kOffMisc = kOffBars + kBars * 8;
-    static constexpr int kOffMost = (kOffMisc + 16 + 15) / 16 * 16;      // [tiles][2 halves][128]: the rows' largest scores, later sums
-    static constexpr int kSmem = kOffMost + kTiles * 256 * 4 + 1024;
+    static constexpr int kOffMost = (kOffMisc + 16 + 15) / 16 * 16;      // [tiles][2 halves][128]: the rows' largest scores, then as many sums
+    static constexpr int kSmem = kOffMost + 2 * kTiles * 256 * 4 + 1024;
     static constexpr int kThreads = kTiles * 256 + 64;
     static constexpr uint32_t kCols = kTiles == 2 ? 512 : 256;
     // tensor memory: scores, weights, outputs; one row tile: the weights of each half of the keys over its scores
@@ -130,6 +132,28 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b)
         : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return d;
 }
+// v[e] of lane i and v[i] of lane e change places among four lanes
+__device__ __forceinline__ void transpose4(uint4 (&v)[4])
+{
+    const int lane = threadIdx.x & 3;
+#pragma unroll
+    for (int bit = 1; bit <= 2; bit <<= 1) {
+        const bool high = lane & bit;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (e & bit) continue;                                       // the pair v[e], v[e + bit]: one goes, the other stays
+            uint4 &a = v[e], &b = v[e + bit];
+            const uint4 give = high ? a : b;
+            uint4 got;
+            got.x = __shfl_xor_sync(0xffffffffu, give.x, bit);
+            got.y = __shfl_xor_sync(0xffffffffu, give.y, bit);
+            got.z = __shfl_xor_sync(0xffffffffu, give.z, bit);
+            got.w = __shfl_xor_sync(0xffffffffu, give.w, bit);
+            if (high) a = got;
+            else b = got;
+        }
+    }
+}
 // bit e set: e <= last
 __device__ __forceinline__ uint32_t bits_to(int last) { return last < 0 ? 0u : last >= 31 ? 0xFFFFFFFFu : (2u << last) - 1u; }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
@@ -138,9 +162,44 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
     return *reinterpret_cast<const uint32_t *>(&b);
 }
 
+// What a block does at a time: its row tiles of a problem and KV head, against its share of the key tiles.
+struct Item {
+    int b, h, first, n, len;     // problem, KV head; the problem's tokens and cached rows
+    int t0, t1;                  // its first and last token, from the problem's first
+    int split, i0, T;            // its key tiles: [i0, i0 + T) of `keys`
+    KeyTiles keys;
+    // The n-th item of this block: there and back over the blocks, so that those in front do not always have the most keys.
+    __device__ static __forceinline__ int index(int n) { return n * (int)gridDim.x + ((n & 1) ? (int)(gridDim.x - 1 - blockIdx.x) : (int)blockIdx.x); }
+};
+// The last tokens see the most keys: they come first, of all problems.  False: no rows.
+__device__ __forceinline__ bool load_item(const RowsParams &p, int idx, int items, int tokens, int pieces, bool tell, Item *x)
+{
+    if (idx >= items) return false;
+    x->split = idx % p.splits;
+    idx /= p.splits;
+    const int pairs = p.hkv * p.tokens.count, pair = idx % pairs;
+    x->h = pair % p.hkv;
+    x->b = pair / p.hkv;
+    x->n = token_span(p.tokens, x->b, &x->first);
+    x->len = p.lens[x->b];
+    if (x->n < 0 || x->len < 0 || x->len > p.cap || (p.causal && x->len < x->n)) {
+        if (tell) report(p.status, RKV_ERR_INVALID_ARG);
+        x->len = 0;
+    }
+    x->t0 = (pieces - 1 - idx / pairs) * tokens;
+    if (x->n <= 0 || x->t0 >= x->n) return false;
+    x->t1 = min(x->n, x->t0 + tokens) - 1;
+    x->keys = key_tiles(p.causal, p.window, p.sinks, x->len, x->n, x->t0, x->t1);
+    if (x->len == 0) x->keys.count = 0;
+    const int per = (x->keys.count + p.splits - 1) / p.splits;
+    x->i0 = x->split * per;
+    x->T = max(0, min(x->keys.count, x->i0 + per) - x->i0);
+    return true;
+}
+
 template <int kDim, int kTiles>
 __global__ void __launch_bounds__(RowsShape<kDim, kTiles>::kThreads, kTiles == 2 ? 1 : 2)
-rows_tc_kernel(RowsParams p, int tokens_per_tile, int blocks_per_problem, const __grid_constant__ CUtensorMap map_k,
+rows_tc_kernel(RowsParams p, int tokens_per_tile, int pieces, int items, const __grid_constant__ CUtensorMap map_k,
                const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_q)
 {
     using S = RowsShape<kDim, kTiles>;
@@ -154,29 +213,6 @@ rows_tc_kernel(RowsParams p, int tokens_per_tile, int blocks_per_problem, const 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     constexpr int kProducer = kTiles * 8, kIssuer = kProducer + 1;
 
-    pdl_wait();
-    // ---- the block's rows.  Without a window the last tokens see the most keys: they come first, of all problems
-    int x = blockIdx.x;
-    const int split = x % p.splits;
-    x /= p.splits;
-    const int pairs = p.hkv * p.tokens.count;
-    const int piece = p.window > 0 ? x % blocks_per_problem : blocks_per_problem - 1 - x / pairs;
-    const int pair = p.window > 0 ? x / blocks_per_problem : x % pairs;
-    const int h = pair % p.hkv, b = pair / p.hkv;
-    int first;
-    const int n = token_span(p.tokens, b, &first);
-    int len = p.lens[b];
-    if (n < 0 || len < 0 || len > p.cap || (p.causal && len < n)) {
-        if (threadIdx.x == 0) report(p.status, RKV_ERR_INVALID_ARG);
-        len = 0;
-    }
-    const int t0 = piece * kTiles * tokens_per_tile;                     // first token of the block
-    if (n <= 0 || t0 >= n) return;
-    const int t1 = min(n, t0 + kTiles * tokens_per_tile) - 1;            // its last
-    KeyTiles keys = key_tiles(p.causal, p.window, p.sinks, len, n, t0, t1);
-    if (len == 0) keys.count = 0;
-    const int per = (keys.count + p.splits - 1) / p.splits, i0 = split * per, T = max(0, min(keys.count, i0 + per) - i0);
-
     if (threadIdx.x == 0) {
         for (int s = 0; s < S::kStages; ++s) {
             mbar_init(bar(S::kFull + s), 1);
@@ -189,10 +225,15 @@ rows_tc_kernel(RowsParams p, int tokens_per_tile, int blocks_per_problem, const 
             mbar_init(bar(S::kWeights + i), 256);
             mbar_init(bar(S::kOut + i), 1);
             mbar_init(bar(S::kRead + i), 256);
+            mbar_init(bar(S::kFree + i), 256);
         }
+        mbar_init(bar(S::kQFree), 1);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (warp == kProducer && lane == 0)
+        for (const CUtensorMap *m : {&map_q, &map_k, &map_v}) prefetch_map(m);
+    pdl_wait();
     if (warp == kIssuer) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
                      ::"r"(smem_u32(tmem_holder)), "r"(S::kCols) : "memory");
@@ -208,100 +249,121 @@ rows_tc_kernel(RowsParams p, int tokens_per_tile, int blocks_per_problem, const 
 
     if (warp == kProducer) {
         // ------------------------------------------------------------------ TMA producer
-        const int head = b * p.hkv + h;
-        if (lane == 0 && T > 0) {
-            mbar_expect_tx(bar(S::kQ), kTiles * S::kHalves * 128 * tokens_per_tile * p.group);
-            for (int i = 0; i < kTiles; ++i)
-                for (int half = 0; half < S::kHalves; ++half)
-                    tma_load_3d(sbase + i * S::kTileBytes + half * S::kBox, &map_q, 64 * half, h * p.group, first + t0 + i * tokens_per_tile,
-                                bar(S::kQ));
-        }
-        int borders = 0;
+        int base = 0, turn = 0, borders = 0;                             // tiles through the ring, items with keys, border tiles so far
         bool ok = true;
-        for (int i = 0; i < 2 * T && ok; ++i) {
-            const bool value = S::value_at(i, T);
-            const int t = keys.tile(i0 + S::index_at(i, T)), s = i % S::kStages, j0 = t * kTile;
-            // rows that nobody sees: at or behind hi, or between the first ones and lo
-            const bool border = value && (j0 + kTile > keys.hi || (j0 < keys.lo && j0 + kTile > keys.sinks));
-            const long long start = rows_tile_start(p, head, t);
-            if (start < 0 && lane == 0) report(p.status, RKV_ERR_INVALID_ARG);
-            const int y = start < 0 ? -kTile : (int)start;               // (beyond the tensor: zeros)
-            ok = mbar_wait(bar(S::kEmpty + s), ((i / S::kStages) & 1) ^ 1, abort_flag, sink);
-            ok = __all_sync(0xffffffffu, ok);
-            if (!ok) break;
-            const uint32_t dst = sbase + S::kOffRing + s * S::kTileBytes, full = border ? bar(S::kBorder) : bar(S::kFull + s);
-            if (lane == 0) {
-                mbar_expect_tx(full, S::kTileBytes);
-                for (int half = 0; half < S::kHalves; ++half) tma_load_2d(dst + half * S::kBox, value ? &map_v : &map_k, 64 * half, y, full);
+        for (int nth = 0; nth * (int)gridDim.x < items && ok; ++nth) {
+            Item x;
+            if (!load_item(p, Item::index(nth), items, kTiles * tokens_per_tile, pieces, lane == 0, &x) || x.T == 0) continue;
+            const int head = x.b * p.hkv + x.h;
+            // what the call sees of this cache: rows [lo, len), and below the first ones
+            const int lo = p.causal && p.window > 0 ? max(0, x.len - x.n + 1 - p.window) : 0;
+            ok = mbar_wait(bar(S::kQFree), (turn & 1) ^ 1, abort_flag, sink);
+            if (lane == 0 && ok) {
+                mbar_expect_tx(bar(S::kQ), kTiles * S::kHalves * 128 * tokens_per_tile * p.group);
+                for (int i = 0; i < kTiles; ++i)
+                    for (int half = 0; half < S::kHalves; ++half)
+                        tma_load_3d(sbase + i * S::kTileBytes + half * S::kBox, &map_q, 64 * half, x.h * p.group,
+                                    x.first + x.t0 + i * tokens_per_tile, bar(S::kQ));
             }
-            if (border) {
-                ok = mbar_wait(full, borders++ & 1, abort_flag, sink);
-                ok = __all_sync(0xffffffffu, ok);
+            for (int i = 0; i < 2 * x.T && ok; ++i) {
+                const bool value = S::value_at(i, x.T);
+                const int t = x.keys.tile(x.i0 + S::index_at(i, x.T)), s = (base + i) % S::kStages, j0 = t * kTile;
+                const bool border = value && (j0 + kTile > x.len || (j0 < lo && j0 + kTile > p.sinks));
+                const long long start = rows_tile_start(p, head, t);
+                if (start < 0 && lane == 0) report(p.status, RKV_ERR_INVALID_ARG);
+                const int y = start < 0 ? -kTile : (int)start;           // (beyond the tensor: zeros)
+                ok = __all_sync(0xffffffffu, mbar_wait(bar(S::kEmpty + s), (((base + i) / S::kStages) & 1) ^ 1, abort_flag, sink));
                 if (!ok) break;
-                uint8_t *tile = smem + S::kOffRing + s * S::kTileBytes;
-                for (int r = 0; r < kTile; r += 4) {                     // 8 lanes to a row of a box
-                    const int row = r + (lane >> 3);
-                    if (!keys.wanted(j0 + row))
-                        for (int half = 0; half < S::kHalves; ++half)
-                            *reinterpret_cast<uint4 *>(tile + half * S::kBox + row * 128 + (lane & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+                const uint32_t dst = sbase + S::kOffRing + s * S::kTileBytes, full = border ? bar(S::kBorder) : bar(S::kFull + s);
+                if (lane == 0) {
+                    mbar_expect_tx(full, S::kTileBytes);
+                    for (int half = 0; half < S::kHalves; ++half)
+                        tma_load_2d(dst + half * S::kBox, value ? &map_v : &map_k, 64 * half, y, full);
                 }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar(S::kFull + s));
+                if (border) {
+                    ok = __all_sync(0xffffffffu, mbar_wait(full, borders++ & 1, abort_flag, sink));
+                    if (!ok) break;
+                    uint8_t *tile = smem + S::kOffRing + s * S::kTileBytes;
+                    for (int r = 0; r < kTile; r += 4) {                 // 8 lanes to a row of a box
+                        const int row = r + (lane >> 3);
+                        if (j0 + row >= x.len || (j0 + row < lo && j0 + row >= p.sinks))
+                            for (int half = 0; half < S::kHalves; ++half)
+                                *reinterpret_cast<uint4 *>(tile + half * S::kBox + row * 128 + (lane & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(S::kFull + s));
+                }
             }
+            base += 2 * x.T;
+            ++turn;
         }
         __syncwarp();
     } else if (warp == kIssuer) {
         // ------------------------------------------------------------------ MMA issuer
         // The whole warp goes through the loop and the waits, so that descriptors stay in uniform registers; one elected lane issues.  (With
         // the loop in one lane's branch a product of 16 took 65 to 85 cycles to issue, twice what it takes to run.)
-        if (T > 0) {
-            const bool leader = elect_one();
-            const uint32_t idesc_s = instr_desc(kTile, kTile), idesc_o = instr_desc(kTile, kDim) | (1u << 16);      // V: keys along K
-            const uint64_t q_desc = smem_desc(sbase), k_desc = smem_desc(sbase + S::kOffRing);
-            // V: 64 columns to a box, boxes kBox apart; 8 keys every 1024 bytes
-            const uint64_t v_desc = (uint64_t)(((sbase + S::kOffRing) & 0x3FFFFu) >> 4) | ((uint64_t)(S::kBox >> 4) << 16) |
-                                    ((uint64_t)(1024u >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
-            constexpr uint32_t kStep = S::kTileBytes >> 4;               // from stage to stage, in a descriptor's units
-            auto scores = [&](int r, int j, bool free_stage) {
-                const int i = S::place_k(j, T);
-                const uint64_t dq = q_desc + (uint64_t)(r * kStep), dk = k_desc + (uint64_t)((i % S::kStages) * kStep);
-                if (leader) {
+        const bool leader = elect_one();
+        const uint32_t idesc_s = instr_desc(kTile, kTile), idesc_o = instr_desc(kTile, kDim) | (1u << 16);          // V: keys along K
+        const uint64_t q_desc = smem_desc(sbase), k_desc = smem_desc(sbase + S::kOffRing);
+        // V: 64 columns to a box, boxes kBox apart; 8 keys every 1024 bytes
+        const uint64_t v_desc = (uint64_t)(((sbase + S::kOffRing) & 0x3FFFFu) >> 4) | ((uint64_t)(S::kBox >> 4) << 16) |
+                                ((uint64_t)(1024u >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+        constexpr uint32_t kStep = S::kTileBytes >> 4;                   // from stage to stage, in a descriptor's units
+        int base = 0, steps = 0, turn = 0;                               // tiles through the ring, key tiles, items with keys so far
+        bool ok = true;
+        int T = 0;
+        auto scores = [&](int r, int j) {
+            const int i = base + S::place_k(j, T);
+            const uint64_t dq = q_desc + (uint64_t)(r * kStep), dk = k_desc + (uint64_t)((i % S::kStages) * kStep);
+            if (leader) {
 #pragma unroll
-                    for (int ks = 0; ks < kDim / 16; ++ks) {
-                        const uint64_t off = (ks >> 2) * (S::kBox >> 4) + (ks & 3) * 2;      // 16 columns further
-                        umma(tmem, dq + off, dk + off, idesc_s, ks > 0 ? 1u : 0u);
-                    }
-                    umma_commit(bar(S::kScores + r));
-                    if (free_stage) umma_commit(bar(S::kEmpty + i % S::kStages));
+                for (int ks = 0; ks < kDim / 16; ++ks) {
+                    const uint64_t off = (ks >> 2) * (S::kBox >> 4) + (ks & 3) * 2;          // 16 columns further
+                    umma(tmem, dq + off, dk + off, idesc_s, ks > 0 ? 1u : 0u);
                 }
-            };
-            auto values = [&](int r, int j, bool free_stage) {
-                const int i = S::place_v(j, T);
-                const uint64_t dv = v_desc + (uint64_t)((i % S::kStages) * kStep);
-                if (leader) {
+                umma_commit(bar(S::kScores + r));
+                if (r == kTiles - 1) {
+                    umma_commit(bar(S::kEmpty + i % S::kStages));
+                    if (j == T - 1) umma_commit(bar(S::kQFree));
+                }
+            }
+        };
+        auto values = [&](int r, int j) {
+            const int i = base + S::place_v(j, T);
+            const uint64_t dv = v_desc + (uint64_t)((i % S::kStages) * kStep);
+            const uint32_t o = tmem + S::kOutCol(0) + r * kDim, w = tmem + S::kWeightCol(0, 0) + r * 64;
+            if (leader) {
 #pragma unroll
-                    for (int ks = 0; ks < kTile / 16; ++ks)              // 16 keys further
-                        umma_ts(tmem + S::kOutCol(r), tmem + S::kWeightCol(r, ks >> 2) + (ks & 3) * 8, dv + (uint64_t)(ks * 128), idesc_o,
-                                ks > 0 ? 1u : (uint32_t)(j > 0));
-                    umma_commit(bar(S::kOut + r));
-                    if (free_stage) umma_commit(bar(S::kEmpty + i % S::kStages));
-                }
-            };
-            auto full = [&](int i) { return mbar_wait(bar(S::kFull + i % S::kStages), (i / S::kStages) & 1, abort_flag, sink); };
-            auto weights = [&](int r, int j) { return mbar_wait(bar(S::kWeights + r), j & 1, abort_flag, sink); };
-            auto read = [&](int r, int j) { return mbar_wait(bar(S::kRead + r), j & 1, abort_flag, sink); };
-            bool ok = mbar_wait(bar(S::kQ), 0, abort_flag, sink) && full(0);
+                for (int ks = 0; ks < kTile / 16; ++ks)                  // 16 keys further
+                    umma_ts(o, w + (ks >> 2) * (S::kWeightCol(0, 1) - S::kWeightCol(0, 0)) + (ks & 3) * 8, dv + (uint64_t)(ks * 128), idesc_o,
+                            ks > 0 ? 1u : (uint32_t)(j > 0));
+                umma_commit(bar(S::kOut + r));
+                if (r == kTiles - 1) umma_commit(bar(S::kEmpty + i % S::kStages));
+            }
+        };
+        Item x;
+        bool any = load_item(p, Item::index(0), items, kTiles * tokens_per_tile, pieces, false, &x);
+        for (int nth = 0; nth * (int)gridDim.x < items && ok; ++nth) {
+            T = any ? x.T : 0;
+            any = load_item(p, Item::index(nth + 1), items, kTiles * tokens_per_tile, pieces, false, &x);        // (on its way meanwhile)
+            if (T == 0) continue;
+            auto full = [&](int i) { return mbar_wait(bar(S::kFull + (base + i) % S::kStages), ((base + i) / S::kStages) & 1, abort_flag, sink); };
+            auto weights = [&](int r, int j) { return mbar_wait(bar(S::kWeights + r), (steps + j) & 1, abort_flag, sink); };
+            auto read = [&](int r, int j) { return mbar_wait(bar(S::kRead + r), (steps + j) & 1, abort_flag, sink); };
+            auto out_free = [&](int r) { return mbar_wait(bar(S::kFree + r), (turn & 1) ^ 1, abort_flag, sink); };       // the item's before
+            ok = mbar_wait(bar(S::kQ), turn & 1, abort_flag, sink) && full(0);
+            // (the accumulator's last scores have been read: their weights have been waited for)
             tc_fence_after();
-            if (ok) scores(0, 0, kTiles == 1);
+            if (ok) scores(0, 0);
             if constexpr (kTiles == 1) {
                 for (int j = 0; j < T && ok; ++j) {
-                    if (!(ok = full(2 * j + 1) && weights(0, j))) break;
+                    if (!(ok = full(2 * j + 1) && weights(0, j) && (j > 0 || out_free(0)))) break;
                     tc_fence_after();
-                    values(0, j, true);
+                    values(0, j);
                     if (j + 1 == T) break;
                     if (!(ok = full(2 * j + 2))) break;
-                    scores(0, j + 1, true);
+                    scores(0, j + 1);
                 }
             } else {
                 // A wait costs some 100 cycles even where nothing is left to wait for: one between any two products, which the product before
@@ -309,16 +371,27 @@ rows_tc_kernel(RowsParams p, int tokens_per_tile, int blocks_per_problem, const 
                 for (int j = 0; j <= T && ok; ++j) {
                     if (!(ok = j < T ? read(0, j) : weights(0, j - 1))) break;
                     tc_fence_after();
-                    if (j < T) scores(1, j, true);
+                    if (j < T) scores(1, j);
                     if (j + 1 < T && !(ok = full(S::place_k(j + 1, T)))) break;
-                    if (j > 0) values(0, j - 1, false);
+                    if (j == 1) {
+                        if (!(ok = out_free(0))) break;
+                        tc_fence_after();
+                    }
+                    if (j > 0) values(0, j - 1);
                     if (!(ok = j < T ? read(1, j) : weights(1, j - 1))) break;
                     tc_fence_after();
-                    if (j + 1 < T) scores(0, j + 1, false);
+                    if (j + 1 < T) scores(0, j + 1);
                     if (j < T && !(ok = full(S::place_v(j, T)))) break;
-                    if (j > 0) values(1, j - 1, true);
+                    if (j == 1) {
+                        if (!(ok = out_free(1))) break;
+                        tc_fence_after();
+                    }
+                    if (j > 0) values(1, j - 1);
                 }
             }
+            base += 2 * T;
+            steps += T;
+            ++turn;
         }
         __syncwarp();
     } else {
@@ -328,138 +401,167 @@ rows_tc_kernel(RowsParams p, int tokens_per_tile, int blocks_per_problem, const 
         const uint32_t s_col = lanes + 64 * half, w_col = lanes + S::kWeightCol(r, half), o_col = lanes + S::kOutCol(r) + half * (kDim / 2);
         float *mosts = reinterpret_cast<float *>(smem + S::kOffMost) + r * 256;
         auto pair_sync = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(1 + r * 4 + (warp & 3)) : "memory"); };       // the two warps of 32 rows
-        const int tt0 = t0 + r * tokens_per_tile, tt1 = min(t1, tt0 + tokens_per_tile - 1);
-        const int t = tt0 + row / p.group, g = row % p.group;
-        const bool mine = row < tokens_per_tile * p.group && t <= t1;    // else: nobody's row, computed and dropped
-        // the cached rows that this row sees, and what all rows of the tile see
-        const int at = len - n + t, last = p.causal ? at : len - 1, from = p.causal && p.window > 0 ? at + 1 - p.window : 0;
-        const int last_all = p.causal ? len - n + tt0 : len - 1, from_all = p.causal && p.window > 0 ? len - n + tt1 + 1 - p.window : 0;
         const float c2 = 1.4426950408889634f * rsqrtf((float)kDim);
-        float m = -INFINITY, l = 0.f;                                    // reference of the weights (raw scores), sum of this thread's weights
+        int steps = 0;                                                   // key tiles so far
         bool ok = true;
-        for (int j = 0; j < T; ++j) {
-            if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bar(S::kScores + r), j & 1, abort_flag, sink));
-            if (!ok) {                                                   // (every warp comes to every one of its pair's barriers)
-                pair_sync();
-                continue;
+        for (int nth = 0; nth * (int)gridDim.x < items; ++nth) {
+            // what the loop needs; the rest is looked up once more behind it, in registers that the scores take until then
+            int T, i0, sink_tiles, first_tile, last, from, last_all, from_all;
+            {
+                Item x;
+                if (!load_item(p, Item::index(nth), items, kTiles * tokens_per_tile, pieces, false, &x)) continue;
+                T = x.T, i0 = x.i0, sink_tiles = x.keys.sink_tiles, first_tile = x.keys.first;
+                // the cached rows that this row sees, and what all rows of the tile see
+                const int tt0 = x.t0 + r * tokens_per_tile, at0 = x.len - x.n + tt0, at = at0 + row / p.group;
+                const int at1 = x.len - x.n + min(x.t1, tt0 + tokens_per_tile - 1);
+                last = p.causal ? at : x.len - 1, from = p.causal && p.window > 0 ? at + 1 - p.window : 0;
+                last_all = p.causal ? at0 : x.len - 1, from_all = p.causal && p.window > 0 ? at1 + 1 - p.window : 0;
             }
-            tc_fence_after();
-            uint32_t s[2][32];
-            tmem_ld32(s_col, s[0]);
-            tmem_ld32(s_col + 32, s[1]);
-            tmem_wait32(s[0]);
-            tmem_wait32(s[1]);
-            if (kTiles == 2) {                                           // the accumulator is the other tile's
-                tc_fence_before();
-                mbar_arrive(bar(S::kRead + r));
-            }
-            const int j0 = keys.tile(i0 + j) * kTile + 64 * half;
-            if (!(j0 + 63 <= last_all && (j0 >= from_all || j0 + 64 <= p.sinks))) {
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    const int k0 = j0 + 32 * c;
-                    const uint32_t sees = bits_to(last - k0) & (~bits_to(from - 1 - k0) | bits_to(p.sinks - 1 - k0));
-#pragma unroll
-                    for (int e = 0; e < 32; ++e)
-                        if (!(sees & (1u << e))) s[c][e] = 0xFF800000u;  // -inf
+            float m = -INFINITY, l = 0.f;                                    // reference of the weights (raw scores), sum of this thread's weights
+            for (int j = 0; j < T; ++j) {
+                if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bar(S::kScores + r), (steps + j) & 1, abort_flag, sink));
+                if (!ok) {                                                   // (every warp comes to every one of its pair's barriers)
+                    pair_sync();
+                    continue;
                 }
-            }
-            float top[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t *x = &s[i >> 1][(i & 1) * 16];
-                top[i] = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
-#pragma unroll
-                for (int e = 2; e < 16; e += 2) top[i] = max3(top[i], __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
-            }
-            float most = max3(fmaxf(top[0], top[1]), top[2], top[3]);
-            // (written again with the next scores, which come when all threads have handed in these weights)
-            mosts[half * 128 + row] = most;
-            pair_sync();
-            most = fmaxf(most, mosts[(half ^ 1) * 128 + row]);
-            const bool outgrown = (most - m) * c2 > kSlack || (m == -INFINITY && most > -INFINITY);
-            if (__any_sync(0xffffffffu, outgrown)) {
-                const float next = outgrown ? most : m, shrink = outgrown ? exp2f((m - next) * c2) : 1.f;
-                m = next;
-                l *= shrink;
-                if (j > 0) {
-                    // all products so far are through (one row tile: they were before these scores): O is the row's threads' to change, a half each
-                    if (kTiles == 2) {
-                        ok = __all_sync(0xffffffffu, mbar_wait(bar(S::kOut + r), (j - 1) & 1, abort_flag, sink));
-                        tc_fence_after();
-                    }
-#pragma unroll 1
-                    for (int c = 0; c < kDim / 2; c += 8) {              // (few registers at a time: the scores stay in theirs)
-                        uint32_t o[8];
-                        tmem_ld8(o_col + c, o);
-                        tmem_wait8(o);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * shrink);
-                        tmem_st8(o_col + c, o);
-                    }
-                }
-            }
-            const float base = m == -INFINITY ? 0.f : -m * c2;
-            const float2 scale = make_float2(c2, c2), shift = make_float2(base, base);
-            float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-            uint32_t w[2][16];
-#pragma unroll
-            for (int c = 0; c < 2; ++c)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    float2 y = fma2(make_float2(__uint_as_float(s[c][2 * e]), __uint_as_float(s[c][2 * e + 1])), scale, shift);
-                    y = make_float2(exp2_approx(y.x), exp2_approx(y.y));
-                    sum[e & 1] = add2(sum[e & 1], y);
-                    w[c][e] = pack_bf16(y.x, y.y);
-                }
-            if (kTiles == 2 && j > 0 && ok) {                            // the weights before these have been read
-                ok = __all_sync(0xffffffffu, mbar_wait(bar(S::kOut + r), (j - 1) & 1, abort_flag, sink));
                 tc_fence_after();
-            }
-            tmem_st16(w_col, w[0]);
-            tmem_st16(w_col + 16, w[1]);
-            sum[0] = add2(sum[0], sum[1]);
-            l += sum[0].x + sum[0].y;
-            tmem_st_wait();
-            tc_fence_before();
-            mbar_arrive(bar(S::kWeights + r));
-        }
-        if (ok && T > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar(S::kOut + r), (T - 1) & 1, abort_flag, sink));
-        mosts[half * 128 + row] = l;
-        pair_sync();
-        l += mosts[(half ^ 1) * 128 + row];
-        tc_fence_after();
-        const int qh = h * p.group + g, c0 = half * (kDim / 2);
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        float *part = p.part ? p.part + (((size_t)(first + t) * p.hq + qh) * p.slots + p.slot + split) * (kDim + 2) : nullptr;
-        __nv_bfloat16 *out = p.part ? nullptr : static_cast<__nv_bfloat16 *>(p.out) + (first + t) * p.out_stride + (size_t)qh * kDim;
+                uint32_t s[2][32];
+                tmem_ld32(s_col, s[0]);
+                tmem_ld32(s_col + 32, s[1]);
+                tmem_wait32(s[0]);
+                tmem_wait32(s[1]);
+                if (kTiles == 2) {                                           // the accumulator is the other tile's
+                    tc_fence_before();
+                    mbar_arrive(bar(S::kRead + r));
+                }
+                const int j0 = (i0 + j < sink_tiles ? i0 + j : first_tile + i0 + j - sink_tiles) * kTile + 64 * half;
+                if (!(j0 + 63 <= last_all && (j0 >= from_all || j0 + 64 <= p.sinks))) {
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        const int k0 = j0 + 32 * c;
+                        const uint32_t sees = bits_to(last - k0) & (~bits_to(from - 1 - k0) | bits_to(p.sinks - 1 - k0));
+                        if (__all_sync(0xffffffffu, sees == 0xFFFFFFFFu)) continue;
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if (!(sees & (1u << e))) s[c][e] = 0xFF800000u;  // -inf
+                    }
+                }
+                float top[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t *x = &s[i >> 1][(i & 1) * 16];
+                    top[i] = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+#pragma unroll
+                    for (int e = 2; e < 16; e += 2) top[i] = max3(top[i], __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
+                }
+                float most = max3(fmaxf(top[0], top[1]), top[2], top[3]);
+                // (written again with the next scores, which come when all threads have handed in these weights)
+                mosts[half * 128 + row] = most;
+                pair_sync();
+                most = fmaxf(most, mosts[(half ^ 1) * 128 + row]);
+                const bool outgrown = (most - m) * c2 > kSlack || (m == -INFINITY && most > -INFINITY);
+                if (__any_sync(0xffffffffu, outgrown)) {
+                    const float next = outgrown ? most : m, shrink = outgrown ? exp2f((m - next) * c2) : 1.f;
+                    m = next;
+                    l *= shrink;
+                    if (j > 0) {
+                        // all products so far are through (one row tile: they were before these scores): O is the row's threads' to change, a half each
+                        if (kTiles == 2) {
+                            ok = __all_sync(0xffffffffu, mbar_wait(bar(S::kOut + r), (steps + j - 1) & 1, abort_flag, sink));
+                            tc_fence_after();
+                        }
 #pragma unroll 1
-        for (int c = 0; c < kDim / 2; c += 32) {
-            uint32_t o[32];
-            if (T > 0 && ok) {
-                tmem_ld32(o_col + c, o);
-                tmem_wait32(o);
-            } else {
+                        for (int c = 0; c < kDim / 2; c += 8) {              // (few registers at a time: the scores stay in theirs)
+                            uint32_t o[8];
+                            tmem_ld8(o_col + c, o);
+                            tmem_wait8(o);
 #pragma unroll
-                for (int e = 0; e < 32; ++e) o[e] = 0u;
+                            for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * shrink);
+                            tmem_st8(o_col + c, o);
+                        }
+                    }
+                }
+                const float base = m == -INFINITY ? 0.f : -m * c2;
+                const float2 scale = make_float2(c2, c2), shift = make_float2(base, base);
+                float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                uint32_t w[2][16];
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        float2 y = fma2(make_float2(__uint_as_float(s[c][2 * e]), __uint_as_float(s[c][2 * e + 1])), scale, shift);
+                        y = make_float2(exp2_approx(y.x), exp2_approx(y.y));
+                        sum[e & 1] = add2(sum[e & 1], y);
+                        w[c][e] = pack_bf16(y.x, y.y);
+                    }
+                if (kTiles == 2 && j > 0 && ok) {                            // the weights before these have been read
+                    ok = __all_sync(0xffffffffu, mbar_wait(bar(S::kOut + r), (steps + j - 1) & 1, abort_flag, sink));
+                    tc_fence_after();
+                }
+                tmem_st16(w_col, w[0]);
+                tmem_st16(w_col + 16, w[1]);
+                sum[0] = add2(sum[0], sum[1]);
+                l += sum[0].x + sum[0].y;
+                tmem_st_wait();
+                tc_fence_before();
+                mbar_arrive(bar(S::kWeights + r));
             }
-            if (!mine) continue;
-            if (part) {
+            steps += T;
+            Item x;
+            load_item(p, Item::index(nth), items, kTiles * tokens_per_tile, pieces, false, &x);
+            if (ok && T > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar(S::kOut + r), (steps - 1) & 1, abort_flag, sink));
+            tc_fence_after();
+            if (T > 0) {                                                     // (the other thread comes to the next item's when it has read these)
+                float *sums = mosts + kTiles * 256;
+                sums[half * 128 + row] = l;
+                pair_sync();
+                l += sums[(half ^ 1) * 128 + row];
+            }
+            const int t = x.t0 + r * tokens_per_tile + row / p.group, qh = x.h * p.group + row % p.group, c0 = half * (kDim / 2);
+            const bool mine = row < tokens_per_tile * p.group && t <= x.t1;  // else: nobody's row, computed and dropped
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            float *part = p.part ? p.part + (((size_t)(x.first + t) * p.hq + qh) * p.slots + p.slot + x.split) * (kDim + 2) : nullptr;
+            __nv_bfloat16 *out = p.part ? nullptr : static_cast<__nv_bfloat16 *>(p.out) + (x.first + t) * p.out_stride + (size_t)qh * kDim;
+#pragma unroll 1
+            for (int c = 0; c < kDim / 2; c += 32) {
+                uint32_t o[32];
+                if (T > 0 && ok) {
+                    tmem_ld32(o_col + c, o);
+                    tmem_wait32(o);
+                } else {
 #pragma unroll
-                for (int e = 0; e < 32; e += 2) *reinterpret_cast<uint2 *>(part + c0 + c + e) = make_uint2(o[e], o[e + 1]);
-            } else {
+                    for (int e = 0; e < 32; ++e) o[e] = 0u;
+                }
+                if (T > 0 && c + 32 == kDim / 2) {                           // the next item's products may begin
+                    tc_fence_before();
+                    mbar_arrive(bar(S::kFree + r));
+                }
+                if (part) {
+                    if (mine)
 #pragma unroll
-                for (int e = 0; e < 32; e += 8) {
-                    uint4 v;
-                    v.x = pack_bf16(__uint_as_float(o[e]) * inv, __uint_as_float(o[e + 1]) * inv);
-                    v.y = pack_bf16(__uint_as_float(o[e + 2]) * inv, __uint_as_float(o[e + 3]) * inv);
-                    v.z = pack_bf16(__uint_as_float(o[e + 4]) * inv, __uint_as_float(o[e + 5]) * inv);
-                    v.w = pack_bf16(__uint_as_float(o[e + 6]) * inv, __uint_as_float(o[e + 7]) * inv);
-                    *reinterpret_cast<uint4 *>(out + c0 + c + e) = v;
+                        for (int e = 0; e < 32; e += 2) *reinterpret_cast<uint2 *>(part + c0 + c + e) = make_uint2(o[e], o[e + 1]);
+                    continue;
+                }
+                // Four lanes exchange the vectors of their rows, so that a store writes 64 bytes of eight rows, not 16 of 32: the rows lie far apart,
+                // and a store takes a cycle per row.  (Written row by row the output held the next item up by 4000 cycles.)
+                uint4 v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t *y = o + 8 * e;
+                    v[e].x = pack_bf16(__uint_as_float(y[0]) * inv, __uint_as_float(y[1]) * inv);
+                    v[e].y = pack_bf16(__uint_as_float(y[2]) * inv, __uint_as_float(y[3]) * inv);
+                    v[e].z = pack_bf16(__uint_as_float(y[4]) * inv, __uint_as_float(y[5]) * inv);
+                    v[e].w = pack_bf16(__uint_as_float(y[6]) * inv, __uint_as_float(y[7]) * inv);
+                }
+                transpose4(v);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {                            // row e of the four lanes', vector lane % 4
+                    const unsigned long long to = __shfl_sync(0xffffffffu, mine ? reinterpret_cast<unsigned long long>(out) : 0ull, (lane & ~3) + e);
+                    if (to) *reinterpret_cast<uint4 *>(reinterpret_cast<__nv_bfloat16 *>(to) + c0 + c + (lane & 3) * 8) = v[e];
                 }
             }
+            if (mine && part && half == 0) *reinterpret_cast<float2 *>(part + kDim) = make_float2(ok && T > 0 ? m * c2 : -INFINITY, ok ? l : 0.f);
         }
-        if (mine && part && half == 0) *reinterpret_cast<float2 *>(part + kDim) = make_float2(ok && T > 0 ? m * c2 : -INFINITY, ok ? l : 0.f);
     }
 
     // ---------------------------------------------------------------------- common exit
@@ -495,13 +597,14 @@ cudaError_t launch_tc_for(const RowsParams &p, cudaStream_t s)
     if ((e = allow_smem_once(done, dev, rows_tc_kernel<kDim, kTiles>, S::kSmem)) != cudaSuccess) return e;
     const int tokens = kTile / p.group;
     const long long per_problem = ((long long)p.tokens.longest + kTiles * tokens - 1) / (kTiles * tokens);
-    const long long blocks = per_problem * p.hkv * p.tokens.count * p.splits;
-    if (blocks > 0x7fffffffll) return cudaErrorInvalidValue;
+    const long long items = per_problem * p.hkv * p.tokens.count * p.splits, resident = kTiles == 2 ? sms : 2ll * sms;
+    if (items > 0x3fffffffll) return cudaErrorInvalidValue;
     const uint64_t rows = p.block_table ? (uint64_t)p.pool_pages * kTile : (uint64_t)p.tokens.count * p.hkv * p.cap;
     CUtensorMap mk, mv, mq;
     if (!make_map_rows(&mk, p.k, rows, kDim, kTile) || !make_map_rows(&mv, p.v, rows, kDim, kTile) || !make_map_queries(&mq, p, tokens))
         return cudaErrorInvalidValue;
-    return launch_early(rows_tc_kernel<kDim, kTiles>, (unsigned)blocks, S::kThreads, S::kSmem, s, 1, p, tokens, (int)per_problem, mk, mv, mq);
+    return launch_early(rows_tc_kernel<kDim, kTiles>, (unsigned)(items < resident ? items : resident), S::kThreads, S::kSmem, s, 1, p, tokens, (int)per_problem,
+                        (int)items, mk, mv, mq);
 }
 
 }  // namespace
