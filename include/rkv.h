@@ -368,8 +368,9 @@ RKV_API int rkv_append_rotary(const rkv_desc_t *desc, void *k_cache, void *v_cac
  * whose length is invalid or less than its new tokens gives zero rows and RKV_ERR_INVALID_ARG in desc->device_status; so does a page that does not
  * exist, whose rows count as zeros.
  * bf16 and 8-bit caches: bf16 products on the tensor cores, fp32 accumulation and softmax; fp32 caches: fp32 throughout.
- * head_dim 64, 128 or 256, any group.  desc->workspace holds rkv_window_workspace_bytes() (0 for calls that fill the GPU): partial results of calls
- * whose keys are split between blocks.  Enqueues one or two kernels on `stream`.
+ * head_dim 64, 128 or 256, any group.  desc->workspace holds rkv_window_workspace_bytes(): partial results of calls whose keys are split between
+ * blocks (calls of few rows), and a bf16 copy of the rows that a call of several tokens sees of 8-bit caches; often 0.  Enqueues one to three
+ * kernels on `stream`.
  */
 RKV_API size_t rkv_window_workspace_bytes(const rkv_desc_t *desc, int32_t budget, int32_t buffer, const rkv_tokens_t *tokens,
                                           int32_t window, int32_t sinks);
@@ -396,7 +397,7 @@ typedef struct rkv_prefix {
  *               and is recorded as RKV_ERR_INVALID_ARG
  * The sequences' own caches may be compressed, appended to and paged as ever; the prefix is not compressed with them.
  * head_dim, groups, types and arithmetic as rkv_window_attention; rows beyond the lengths are not read.  desc->workspace holds
- * rkv_prefix_workspace_bytes().  Enqueues up to three kernels on `stream`.
+ * rkv_prefix_workspace_bytes() (partial results; a bf16 copy of 8-bit prefixes).  Enqueues up to four kernels on `stream`.
  */
 RKV_API size_t rkv_prefix_workspace_bytes(const rkv_desc_t *desc, int32_t budget, int32_t buffer, const rkv_prefix_t *prefix);
 RKV_API int rkv_prefix_attention(const rkv_desc_t *desc, const void *k_cache, const void *v_cache, const void *q_new,

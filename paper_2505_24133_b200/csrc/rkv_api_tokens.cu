@@ -81,9 +81,20 @@ int splits_for(const rkv_desc_t *d, const RowsParams &p)
     const int tiles = rows_sm100_tiles(p);
     return rows_splits(p, tiles * (kTile / p.group), tiles == 2 ? sms : 2 * sms, 1.6);
 }
-cudaError_t launch_rows(const rkv_desc_t *d, const RowsParams &p, cudaStream_t s)
+// Room for the bf16 copy of what a call of the tensor-core kernel sees of 8-bit caches.
+size_t wide_bytes(const rkv_desc_t *d, const RowsParams &p)
 {
-    return on_tensor_cores(d) ? launch_rows_sm100(p, s) : launch_rows_simt(p, d->dtype, s);
+    if (d->dtype != RKV_FP8_E4M3 || !on_tensor_cores(d)) return 0;
+    return (size_t)p.tokens.count * p.hkv * tiles_seen(p, p.tokens.longest) * kTile * p.d * 2 * sizeof(__nv_bfloat16);
+}
+cudaError_t launch_rows(const rkv_desc_t *d, RowsParams p, void *wide, cudaStream_t s)
+{
+    if (!on_tensor_cores(d)) return launch_rows_simt(p, d->dtype, s);
+    if (d->dtype == RKV_FP8_E4M3) {
+        const cudaError_t e = launch_rows_widen(&p, wide, (int)tiles_seen(p, p.tokens.longest), s);
+        if (e != cudaSuccess) return e;
+    }
+    return launch_rows_sm100(p, s);
 }
 size_t part_bytes(const RowsParams &p) { return align_up((size_t)p.tokens.total * p.hq * p.slots * (p.d + 2) * sizeof(float), 256); }
 
@@ -113,7 +124,7 @@ void fill_rows(const rkv_desc_t *d, int cap, RowsParams *p)
 struct Plan {
     RowsParams rows;
     bool single, separate;       // separate: its splits are blocks of their own
-    size_t bytes;
+    size_t wide, bytes;          // workspace: the partial results, then from `wide` on the copies of 8-bit caches
 };
 bool back_to_back(const rkv_desc_t *d, int64_t stride) { return stride == 0 || stride == (int64_t)d->n_q_heads * d->head_dim; }
 
@@ -137,10 +148,11 @@ int plan_window(const rkv_desc_t *d, int budget, int buffer, const rkv_tokens_t 
     if (x->single) {
         attend_more_plan(p, d->dtype, tiles, sm_count(), &x->separate);
         p->slots = x->separate ? p->splits : 0;
-        x->bytes = x->separate ? part_bytes(*p) : 0;
+        x->wide = x->bytes = x->separate ? part_bytes(*p) : 0;
     } else {
         p->splits = p->slots = splits_for(d, *p);
-        x->bytes = p->slots > 1 ? part_bytes(*p) : 0;
+        x->wide = p->slots > 1 ? part_bytes(*p) : 0;
+        x->bytes = x->wide + wide_bytes(d, *p);
     }
     return RKV_OK;
 }
@@ -176,7 +188,8 @@ int plan_prefix(const rkv_desc_t *d, int budget, int buffer, const rkv_prefix_t 
     else p->splits = splits_for(d, *p);
     p->slot = shared->splits;
     shared->slots = p->slots = shared->splits + (own->single && !own->separate ? 0 : p->splits);
-    own->bytes = part_bytes(*p);
+    own->wide = part_bytes(*p);
+    own->bytes = own->wide + wide_bytes(d, *shared) + (own->single ? 0 : wide_bytes(d, *p));
     return RKV_OK;
 }
 
@@ -256,9 +269,10 @@ int rkv_window_attention(const rkv_desc_t *d, const void *k_cache, const void *v
     p.v = v_cache;
     p.lens = seq_lens;
     p.out = out;
-    p.part = x.bytes ? static_cast<float *>(d->workspace) : nullptr;
+    p.part = x.wide ? static_cast<float *>(d->workspace) : nullptr;
+    char *wide = static_cast<char *>(d->workspace) + x.wide;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    cudaError_t e = x.single ? launch_attend_more(p, d->dtype, tiles_seen(p, 1), x.separate, 0, false, s) : launch_rows(d, p, s);
+    cudaError_t e = x.single ? launch_attend_more(p, d->dtype, tiles_seen(p, 1), x.separate, 0, false, s) : launch_rows(d, p, wide, s);
     if (e == cudaSuccess && p.part) e = launch_rows_merge(p, d->dtype, s);
     return e == cudaSuccess ? RKV_OK : cuda_fail(e, "window attention launch");
 }
@@ -291,10 +305,11 @@ int rkv_prefix_attention(const rkv_desc_t *d, const void *k_cache, const void *v
         p->part = static_cast<float *>(d->workspace);
     }
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    cudaError_t e = launch_rows(d, shared, s);
+    char *wide = static_cast<char *>(d->workspace) + own.wide;
+    cudaError_t e = launch_rows(d, shared, wide, s);
     if (e == cudaSuccess)
         e = own.single ? launch_attend_more(own.rows, d->dtype, tiles_seen(own.rows, 1), own.separate, shared.splits, true, s)
-                       : launch_rows(d, own.rows, s);
+                       : launch_rows(d, own.rows, wide + wide_bytes(d, shared), s);
     if (e == cudaSuccess && (!own.single || own.separate)) e = launch_rows_merge(own.rows, d->dtype, s);
     return e == cudaSuccess ? RKV_OK : cuda_fail(e, "prefix attention launch");
 }

@@ -255,8 +255,7 @@ rows_tc_kernel(RowsParams p, int tokens_per_tile, int pieces, int items, const _
             Item x;
             if (!load_item(p, Item::index(nth), items, kTiles * tokens_per_tile, pieces, lane == 0, &x) || x.T == 0) continue;
             const int head = x.b * p.hkv + x.h;
-            // what the call sees of this cache: rows [lo, len), and below the first ones
-            const int lo = p.causal && p.window > 0 ? max(0, x.len - x.n + 1 - p.window) : 0;
+            const CallTiles call = call_tiles(p.causal, p.window, p.sinks, x.len, x.n);
             ok = mbar_wait(bar(S::kQFree), (turn & 1) ^ 1, abort_flag, sink);
             if (lane == 0 && ok) {
                 mbar_expect_tx(bar(S::kQ), kTiles * S::kHalves * 128 * tokens_per_tile * p.group);
@@ -268,8 +267,8 @@ rows_tc_kernel(RowsParams p, int tokens_per_tile, int pieces, int items, const _
             for (int i = 0; i < 2 * x.T && ok; ++i) {
                 const bool value = S::value_at(i, x.T);
                 const int t = x.keys.tile(x.i0 + S::index_at(i, x.T)), s = (base + i) % S::kStages, j0 = t * kTile;
-                const bool border = value && (j0 + kTile > x.len || (j0 < lo && j0 + kTile > p.sinks));
-                const long long start = rows_tile_start(p, head, t);
+                const bool border = value && !p.compact_tiles && (j0 + kTile > x.len || (j0 < call.lo && j0 + kTile > call.sinks));
+                const long long start = p.compact_tiles ? ((long long)head * p.compact_tiles + call.place(t)) * kTile : rows_tile_start(p, head, t);
                 if (start < 0 && lane == 0) report(p.status, RKV_ERR_INVALID_ARG);
                 const int y = start < 0 ? -kTile : (int)start;           // (beyond the tensor: zeros)
                 ok = __all_sync(0xffffffffu, mbar_wait(bar(S::kEmpty + s), (((base + i) / S::kStages) & 1) ^ 1, abort_flag, sink));
@@ -286,7 +285,7 @@ rows_tc_kernel(RowsParams p, int tokens_per_tile, int pieces, int items, const _
                     uint8_t *tile = smem + S::kOffRing + s * S::kTileBytes;
                     for (int r = 0; r < kTile; r += 4) {                 // 8 lanes to a row of a box
                         const int row = r + (lane >> 3);
-                        if (j0 + row >= x.len || (j0 + row < lo && j0 + row >= p.sinks))
+                        if (!call.wanted(j0 + row, x.len))
                             for (int half = 0; half < S::kHalves; ++half)
                                 *reinterpret_cast<uint4 *>(tile + half * S::kBox + row * 128 + (lane & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
                     }
@@ -599,7 +598,8 @@ cudaError_t launch_tc_for(const RowsParams &p, cudaStream_t s)
     const long long per_problem = ((long long)p.tokens.longest + kTiles * tokens - 1) / (kTiles * tokens);
     const long long items = per_problem * p.hkv * p.tokens.count * p.splits, resident = kTiles == 2 ? sms : 2ll * sms;
     if (items > 0x3fffffffll) return cudaErrorInvalidValue;
-    const uint64_t rows = p.block_table ? (uint64_t)p.pool_pages * kTile : (uint64_t)p.tokens.count * p.hkv * p.cap;
+    const uint64_t rows = p.block_table ? (uint64_t)p.pool_pages * kTile
+                                        : (uint64_t)p.tokens.count * p.hkv * (p.compact_tiles ? p.compact_tiles * kTile : p.cap);
     CUtensorMap mk, mv, mq;
     if (!make_map_rows(&mk, p.k, rows, kDim, kTile) || !make_map_rows(&mv, p.v, rows, kDim, kTile) || !make_map_queries(&mq, p, tokens))
         return cudaErrorInvalidValue;
@@ -609,7 +609,7 @@ cudaError_t launch_tc_for(const RowsParams &p, cudaStream_t s)
 
 }  // namespace
 
-bool rows_sm100_supported(int dtype, int d, int group) { return dtype == RKV_BF16 && (d == 64 || d == 128) && group <= kTile; }
+bool rows_sm100_supported(int dtype, int d, int group) { return dtype != RKV_F32 && (d == 64 || d == 128) && group <= kTile; }
 
 // Two row tiles to a block where a problem has more than one.
 int rows_sm100_tiles(const RowsParams &p) { return p.tokens.longest > kTile / p.group ? 2 : 1; }

@@ -54,6 +54,7 @@ struct RowsParams {
     TokenMap tokens;                // count = problems
     int hkv, hq, group, d, cap;
     int causal, window, sinks;      // causal: token t of n stands in row len - n + t and sees rows up to its own; else every token sees all rows
+    int compact_tiles;              // > 0: k and v are [count][hkv][compact_tiles][128][d], the tiles that the call sees (CallTiles), in turn
     int splits, slot, slots;        // blocks that share a row tile's keys; their partial results are slots slot .. of the rows' `slots`
     float *part;                    // [total * hq][slots][d + 2]: weighted sum, maximum (base 2), sum of weights; null: `out` is written
     void *out;
@@ -79,6 +80,18 @@ __device__ __forceinline__ KeyTiles key_tiles(int causal, int window, int sinks,
     if (k.hi <= 0) k.count = 0;
     return k;
 }
+// The same for all tokens of a problem: rows [0, sinks) and [lo, len).
+struct CallTiles {
+    int sink_tiles, first, count, lo, sinks;
+    __device__ __forceinline__ int tile(int i) const { return i < sink_tiles ? i : first + i - sink_tiles; }
+    __device__ __forceinline__ int place(int t) const { return t < sink_tiles ? t : sink_tiles + t - first; }
+    __device__ __forceinline__ bool wanted(int row, int len) const { return row < sinks || (row >= lo && row < len); }
+};
+__device__ __forceinline__ CallTiles call_tiles(int causal, int window, int sinks, int len, int n)
+{
+    const KeyTiles k = key_tiles(causal, window, sinks, len, n, 0, n - 1);
+    return CallTiles{k.sink_tiles, k.first, k.count, k.lo, k.sinks};
+}
 // Rows of a cache: where 128-row tile t of a head starts, or -1 for a page that does not exist.
 __device__ __forceinline__ long long rows_tile_start(const RowsParams &p, int head, int t)
 {
@@ -86,6 +99,8 @@ __device__ __forceinline__ long long rows_tile_start(const RowsParams &p, int he
     const int page = p.block_table[(size_t)head * (p.cap / kTile) + t];
     return page < 0 || page >= p.pool_pages ? -1 : (long long)page * kTile;
 }
+// 8-bit caches: the tiles that a call sees, as bf16, rows that it does not see as zeros; `wide` holds K's, then V's.  `p` becomes the call on them.
+cudaError_t launch_rows_widen(RowsParams *p, void *wide, int tiles, cudaStream_t s);
 cudaError_t launch_rows_simt(const RowsParams &p, int dtype, cudaStream_t s);
 bool rows_sm100_supported(int dtype, int d, int group);
 int rows_sm100_tiles(const RowsParams &p);                  // row tiles of a block
