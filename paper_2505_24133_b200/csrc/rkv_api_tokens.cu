@@ -74,10 +74,12 @@ int rows_splits(const RowsParams &p, int tokens_per_block, long long resident, d
     return (int)best;
 }
 bool on_tensor_cores(const rkv_desc_t *d) { return rows_sm100_supported(d->dtype, d->head_dim, d->n_q_heads / d->n_kv_heads); }
-int splits_for(const rkv_desc_t *d, const RowsParams &p)
+int splits_for(const rkv_desc_t *d, const RowsParams &p, long long sms)
 {
-    const long long sms = sm_count();
-    if (!on_tensor_cores(d)) return rows_splits(p, p.group >= kSimtRows ? 1 : kSimtRows / p.group, 2 * sms, 12.0);
+    if (!on_tensor_cores(d)) {
+        const int rows = rows_simt_rows(p);
+        return rows_splits(p, p.group >= rows ? 1 : rows / p.group, 2 * sms, rows == 16 ? 4.0 : 12.0);
+    }
     const int tiles = rows_sm100_tiles(p);
     return rows_splits(p, tiles * (kTile / p.group), tiles == 2 ? sms : 2 * sms, 1.6);
 }
@@ -96,7 +98,7 @@ cudaError_t launch_rows(const rkv_desc_t *d, RowsParams p, void *wide, cudaStrea
     }
     return launch_rows_sm100(p, s);
 }
-size_t part_bytes(const RowsParams &p) { return align_up((size_t)p.tokens.total * p.hq * p.slots * (p.d + 2) * sizeof(float), 256); }
+size_t part_bytes(const RowsParams &p) { return align_up((size_t)p.tokens.total * p.hq * p.slots * slot_floats(p.d) * sizeof(float), 256); }
 
 int check_room(const rkv_desc_t *d, size_t bytes)
 {
@@ -124,6 +126,8 @@ void fill_rows(const rkv_desc_t *d, int cap, RowsParams *p)
 struct Plan {
     RowsParams rows;
     bool single, separate;       // separate: its splits are blocks of their own
+    bool joined;                 // single: the kernel reads the prefixes itself, for every sequence again
+    long long tiles;             // single: key tiles that a token sees at most
     size_t wide, bytes;          // workspace: the partial results, then from `wide` on the copies of 8-bit caches
 };
 bool back_to_back(const rkv_desc_t *d, int64_t stride) { return stride == 0 || stride == (int64_t)d->n_q_heads * d->head_dim; }
@@ -142,15 +146,15 @@ int plan_window(const rkv_desc_t *d, int budget, int buffer, const rkv_tokens_t 
     p->causal = 1;
     p->window = window;
     p->sinks = sinks;
-    const long long tiles = tiles_seen(*p, 1);
+    const long long tiles = x->tiles = tiles_seen(*p, 1);
     x->single = !tokens->offsets && tokens->longest == 1 && back_to_back(d, tokens->q_stride) && back_to_back(d, tokens->out_stride) &&
                 attend_more_supported(d->dtype, d->head_dim, p->group, tiles);
     if (x->single) {
-        attend_more_plan(p, d->dtype, tiles, sm_count(), &x->separate);
+        attend_more_plan(p, d->dtype, tiles, sm_count(), false, &x->separate);
         p->slots = x->separate ? p->splits : 0;
         x->wide = x->bytes = x->separate ? part_bytes(*p) : 0;
     } else {
-        p->splits = p->slots = splits_for(d, *p);
+        p->splits = p->slots = splits_for(d, *p, sm_count());
         x->wide = p->slots > 1 ? part_bytes(*p) : 0;
         x->bytes = x->wide + wide_bytes(d, *p);
     }
@@ -166,6 +170,8 @@ int check_prefix(const rkv_desc_t *d, const rkv_prefix_t *x)
     return RKV_OK;
 }
 
+constexpr long long kReadAgainBytes = 48ll << 20;
+
 // shared: the prefixes' rows, whose partial results are a row's first slots; own: the sequences'.
 int plan_prefix(const rkv_desc_t *d, int budget, int buffer, const rkv_prefix_t *x, RowsParams *shared, Plan *own)
 {
@@ -179,13 +185,24 @@ int plan_prefix(const rkv_desc_t *d, int budget, int buffer, const rkv_prefix_t 
     shared->block_table = x->table;
     shared->pool_pages = x->pages;
     shared->tokens = TokenMap{nullptr, x->count, d->batch, d->batch / x->count};
-    shared->splits = splits_for(d, *shared);
+    const int sms = sm_count();
     fill_rows(d, budget + buffer, p);
     p->tokens = TokenMap{nullptr, d->batch, d->batch, 1};
-    const long long tiles = tiles_seen(*p, 1);
-    own->single = attend_more_supported(d->dtype, d->head_dim, p->group, tiles);
-    if (own->single) attend_more_plan(p, d->dtype, tiles, sm_count(), &own->separate);
-    else p->splits = splits_for(d, *p);
+    // Prefixes of few rows or few sequences are read again for every sequence, mostly from L2: one kernel instead of two, the second of which
+    // waits for the first.
+    const long long again = (long long)d->batch * d->n_kv_heads * x->rows * 2 * d->head_dim * (d->dtype == RKV_BF16 ? 2 : 1);
+    const long long tiles = tiles_seen(*p, 1), with_prefix = tiles + tiles_seen(*shared, 1);
+    own->joined = (again <= kReadAgainBytes || d->batch == x->count) && attend_more_supported(d->dtype, d->head_dim, p->group, with_prefix);
+    own->tiles = own->joined ? with_prefix : tiles;
+    own->single = own->joined || attend_more_supported(d->dtype, d->head_dim, p->group, tiles);
+    if (own->single) attend_more_plan(p, d->dtype, own->tiles, sms, !own->joined, &own->separate);
+    else p->splits = splits_for(d, *p, sms);
+    if (own->joined) {
+        p->slots = own->separate ? p->splits : 0;
+        own->wide = own->bytes = own->separate ? part_bytes(*p) : 0;
+        return RKV_OK;
+    }
+    shared->splits = splits_for(d, *shared, sms);
     p->slot = shared->splits;
     shared->slots = p->slots = shared->splits + (own->single && !own->separate ? 0 : p->splits);
     own->wide = part_bytes(*p);
@@ -272,7 +289,7 @@ int rkv_window_attention(const rkv_desc_t *d, const void *k_cache, const void *v
     p.part = x.wide ? static_cast<float *>(d->workspace) : nullptr;
     char *wide = static_cast<char *>(d->workspace) + x.wide;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    cudaError_t e = x.single ? launch_attend_more(p, d->dtype, tiles_seen(p, 1), x.separate, 0, false, s) : launch_rows(d, p, wide, s);
+    cudaError_t e = x.single ? launch_attend_more(p, d->dtype, x.tiles, x.separate, 0, false, nullptr, s) : launch_rows(d, p, wide, s);
     if (e == cudaSuccess && p.part) e = launch_rows_merge(p, d->dtype, s);
     return e == cudaSuccess ? RKV_OK : cuda_fail(e, "window attention launch");
 }
@@ -306,10 +323,15 @@ int rkv_prefix_attention(const rkv_desc_t *d, const void *k_cache, const void *v
     }
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     char *wide = static_cast<char *>(d->workspace) + own.wide;
-    cudaError_t e = launch_rows(d, shared, wide, s);
-    if (e == cudaSuccess)
-        e = own.single ? launch_attend_more(own.rows, d->dtype, tiles_seen(own.rows, 1), own.separate, shared.splits, true, s)
-                       : launch_rows(d, own.rows, wide + wide_bytes(d, shared), s);
+    cudaError_t e = cudaSuccess;
+    if (own.joined) {
+        e = launch_attend_more(own.rows, d->dtype, own.tiles, own.separate, 0, false, &shared, s);
+    } else {
+        e = launch_rows(d, shared, wide, s);
+        if (e == cudaSuccess)
+            e = own.single ? launch_attend_more(own.rows, d->dtype, own.tiles, own.separate, shared.splits, true, nullptr, s)
+                           : launch_rows(d, own.rows, wide + wide_bytes(d, shared), s);
+    }
     if (e == cudaSuccess && (!own.single || own.separate)) e = launch_rows_merge(own.rows, d->dtype, s);
     return e == cudaSuccess ? RKV_OK : cuda_fail(e, "prefix attention launch");
 }

@@ -15,15 +15,19 @@ bool attend_more_supported(int dtype, int d, int group, long long tiles)
     return dtype != RKV_F32 && attend_supported(group, dtype, d) && tiles <= (long long)kTcMaxSplits * 2 * kTcChunkTiles;
 }
 
-// Splits as for rkv_decode_attention; blocks of their own where those are the faster there (attend_tc_separate).
-void attend_more_plan(RowsParams *p, int dtype, long long tiles, int sms, bool *separate)
+// Splits as for rkv_decode_attention; blocks of their own where those are the faster there (attend_tc_separate), and beside another
+// kernel where not all blocks are on the GPU at a time: a block that waited for the other kernel's results would keep the next one out (256
+// sequences of 1152 rows and four prefixes of 16000: 259 us; 64 of 580 and 2048: 60 us).
+void attend_more_plan(RowsParams *p, int dtype, long long tiles, int sms, bool others, bool *separate)
 {
     const int heads = p->tokens.count * p->hkv;
     p->splits = attend_tc_splits(heads, (int)tiles * kTile, sms);
-    *separate = p->splits > 1 && source_of(dtype, p->d) != 0 && (long long)heads * p->splits > 4ll * sms;
+    *separate = others && (long long)heads * p->splits > 2ll * sms;
+    *separate = *separate || p->splits > 1 && source_of(dtype, p->d) != 0 && (long long)heads * p->splits > 4ll * sms;
 }
 
-cudaError_t launch_attend_more(const RowsParams &r, int dtype, long long tiles, bool separate, int others, bool late, cudaStream_t s)
+cudaError_t launch_attend_more(const RowsParams &r, int dtype, long long tiles, bool separate, int others, bool late, const RowsParams *prefix,
+                               cudaStream_t s)
 {
     AttendTcMore p = {};
     p.seq_lens = r.lens;
@@ -46,7 +50,21 @@ cudaError_t launch_attend_more(const RowsParams &r, int dtype, long long tiles, 
     p.others = others;
     p.late = late ? 1 : 0;
     if (p.tiles_per_split > 2 * kTcChunkTiles) return cudaErrorInvalidValue;
-    return launch_tc_group(p, r.k, r.v, r.q, r.tokens.count, r.pool_pages, source_of(dtype, r.d), s);
+    AttendTcMoreMaps maps;
+    p.per_prefix = 1;
+    if (prefix) {
+        p.prefix_lens = prefix->lens;
+        p.prefix_table = prefix->block_table;
+        p.prefix_pages = prefix->pool_pages;
+        p.prefix_cap = prefix->cap;
+        p.per_prefix = prefix->tokens.longest;
+    }
+    // (without prefixes the maps of their tiles are never looked at)
+    const RowsParams &x = prefix ? *prefix : r;
+    const uint64_t rows = x.block_table ? (uint64_t)x.pool_pages * kTile : (uint64_t)x.tokens.count * x.hkv * x.cap;
+    if (!make_cache_map(&maps.prefix_k, x.k, rows, source_of(dtype, r.d)) || !make_cache_map(&maps.prefix_v, x.v, rows, source_of(dtype, r.d)))
+        return cudaErrorInvalidValue;
+    return launch_tc_group(p, maps, r.k, r.v, r.q, r.tokens.count, r.pool_pages, source_of(dtype, r.d), s);
 }
 
 }  // namespace rkv

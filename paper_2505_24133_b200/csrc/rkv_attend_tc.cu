@@ -62,7 +62,7 @@ cudaError_t launch_attend_tc(const void *k_cache, const void *v_cache, const voi
     p.wait_cycles = wait_cycles;
     p.block_table = block_table;
     if (p.tiles_per_split > 2 * kTcChunkTiles) return cudaErrorInvalidValue;
-    return launch_tc_group(p, k_cache, v_cache, q_new, batch, pool_pages, src, s);
+    return launch_tc_group(p, AttendTcMaps(), k_cache, v_cache, q_new, batch, pool_pages, src, s);
 }
 
 }  // namespace rkv

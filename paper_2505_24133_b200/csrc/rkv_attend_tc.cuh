@@ -102,10 +102,24 @@ struct AttendTcMore : AttendTcParams {
     int least;                  // a length below it is an error
     int window, sinks;          // the token sees rows L - window .. L - 1 (0: all) and 0 .. sinks - 1
     long long pool_pages;
-    float *slots;               // [batch][hq][slots_per_row][d + 2]: what other kernels (and, with `separate`, the splits) leave
+    float *slots;               // [batch][hq][slots_per_row][d + 4]: what other kernels (and, with `separate`, the splits) leave
     int slots_per_row, others;  // others: slots 0 .. others - 1 are there when the kernel before this one is done
+    // prefixes that stand in front of the sequences' own rows (as rkv_prefix_t; sequence b has prefix b / per_prefix); prefix_lens null: none
+    const int32_t *prefix_lens, *prefix_table;
+    long long prefix_pages;
+    int prefix_cap, per_prefix;
     int late;                   // everything but those slots and the output was there when this kernel could start
 };
+
+// The tensor maps of a launch.
+struct AttendTcMaps {
+    CUtensorMap k, v, q;
+};
+struct AttendTcMoreMaps : AttendTcMaps {
+    CUtensorMap prefix_k, prefix_v;
+};
+template <class Args>
+using MapsFor = typename std::conditional<std::is_same<Args, AttendTcMore>::value, AttendTcMoreMaps, AttendTcMaps>::type;
 
 __device__ __forceinline__ void tmem_wait16(uint32_t (&r)[16])
 {
@@ -152,12 +166,12 @@ __device__ __forceinline__ uint32_t small_off(int g, int k)
 enum { kPlain, kEarly, kTwo };
 template <int G, int kSrc, int kForm, class Args>
 __global__ void __launch_bounds__(kTcThreads, 2)
-attend_tc_kernel(Args p, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
-                 const __grid_constant__ CUtensorMap map_q)
+attend_tc_kernel(Args p, const __grid_constant__ MapsFor<Args> maps)
 {
     constexpr bool kFp8 = kSrc != 0;            // the tiles pass through the softmax threads on their way to the tensor cores
     constexpr int kDim = kSrc == 2 ? 64 : kHeadDim;          // head dimension of the caches, the queries and the output
     constexpr bool kMore = std::is_same<Args, AttendTcMore>::value;
+    constexpr bool kSeparate = kFp8 || kMore;   // the splits may be blocks of their own
     using Out = typename std::conditional<kMore, __nv_bfloat16, float>::type;
     extern __shared__ uint8_t att_tc_raw[];
     uint8_t *smem = align_smem(att_tc_raw);
@@ -197,7 +211,7 @@ attend_tc_kernel(Args p, const __grid_constant__ CUtensorMap map_k, const __grid
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     if (kForm == kEarly && warp == 4 && lane == 0)
-        for (const CUtensorMap *m : {&map_q, &map_k, &map_v}) prefetch_map(m);
+        for (const CUtensorMap *m : {&maps.q, &maps.k, &maps.v}) prefetch_map(m);
     // the P buffers start as zeros: rows of queries the group does not have are never written (and so does the query
     // operand: with 64 dimensions only its first half is loaded)
     for (int x = threadIdx.x; x < 3 * kTcSmall / 16; x += kTcThreads)
@@ -216,9 +230,19 @@ attend_tc_kernel(Args p, const __grid_constant__ CUtensorMap map_k, const __grid
 
     const int t0 = split * p.tiles_per_split;                       // first key tile of this block
     // where key tile t of the head starts, in rows of the 2-D [rows][d] view of the caches
-    KeyTiles keys;                          // (kMore)
+    KeyTiles keys;                          // (kMore: of the sequence's own rows, behind `prefix_tiles` of its prefix's `prefix_len` rows)
+    int prefix_tiles = 0, prefix_len = 0;
     auto tile_y = [&](int t) -> int {
         if constexpr (kMore) {
+            if (t < prefix_tiles) {
+                const int prefix_head = b / p.per_prefix * p.hkv + h;
+                if (!p.prefix_table) return prefix_head * p.prefix_cap + t * kTile;
+                const int page = p.prefix_table[(size_t)prefix_head * (p.prefix_cap / kTile) + t];
+                if (page >= 0 && page < p.prefix_pages) return page * kTile;
+                report(p.status, RKV_ERR_INVALID_ARG);
+                return -kTile;              // (in front of the tensor: zeros)
+            }
+            t -= prefix_tiles;
             if (!p.block_table) return head * p.cap + keys.tile(t) * kTile;
             const int page = p.block_table[(size_t)head * (p.cap / kTile) + keys.tile(t)];
             if (page >= 0 && page < p.pool_pages) return page * kTile;
@@ -244,12 +268,12 @@ attend_tc_kernel(Args p, const __grid_constant__ CUtensorMap map_k, const __grid
     auto fetch_queries = [&]() {
         mbar_expect_tx(bar(kBarQ), kSrc == 2 ? kTcSmall / 2 : kTcSmall);
         const int qy = b * p.hq + h * G;                 // the group's G query rows (the rows after them are not used)
-        tma_load_2d(sbase + kOffQ, &map_q, 0, qy, bar(kBarQ));
-        if (kSrc != 2) tma_load_2d(sbase + kOffQ + kTcSmall / 2, &map_q, 64, qy, bar(kBarQ));
+        tma_load_2d(sbase + kOffQ, &maps.q, 0, qy, bar(kBarQ));
+        if (kSrc != 2) tma_load_2d(sbase + kOffQ + kTcSmall / 2, &maps.q, 64, qy, bar(kBarQ));
     };
     if (kForm == kEarly && warp == 4 && lane == 0) {
         fetch_queries();
-        if (!kMore) fetch_tile(&map_k, 0, tile_y(t0));       // (which tile is the first depends on the length there)
+        if (!kMore) fetch_tile(&maps.k, 0, tile_y(t0));       // (which tile is the first depends on the length there)
     }
     int L = p.seq_lens[b];
     bool short_of = false;
@@ -262,11 +286,23 @@ attend_tc_kernel(Args p, const __grid_constant__ CUtensorMap map_k, const __grid
     if constexpr (kMore) {
         keys = key_tiles(1, p.window, p.sinks, L, 1, 0, 0);
         tiles = keys.count;
+        if (p.prefix_lens) {
+            prefix_len = p.prefix_lens[b / p.per_prefix];
+            if (prefix_len < 0 || prefix_len > p.prefix_cap) {
+                report(p.status, RKV_ERR_INVALID_ARG);
+                prefix_len = 0;
+            }
+            prefix_tiles = (prefix_len + kTile - 1) / kTile;
+            tiles += prefix_tiles;
+        }
     }
     const int T = min(p.tiles_per_split, tiles - t0);                // its tiles (<= 0: none)
     // row r of the block's tile t is cached and the query sees it
     auto seen = [&](int t, int r) -> bool {
-        if constexpr (kMore) return keys.wanted(keys.tile(t0 + t) * kTile + r);
+        if constexpr (kMore) {
+            if (t0 + t < prefix_tiles) return (t0 + t) * kTile + r < prefix_len;
+            return keys.wanted(keys.tile(t0 + t - prefix_tiles) * kTile + r);
+        }
         return (t0 + t) * kTile + r < L;
     };
     // more than a block's columns hold the scores of: two chunks, one after the other, each with its own maximum and output columns
@@ -281,10 +317,10 @@ attend_tc_kernel(Args p, const __grid_constant__ CUtensorMap map_k, const __grid
     // [G][d + 2]: unnormalised output, maximum (base-2 domain), sum of weights
     float *part = reinterpret_cast<float *>(smem + kOffP);
     int part_stride = kStride, part_max = kHeadDim;
-    if (kFp8 && p.separate) {
+    if (kSeparate && p.separate) {
         if constexpr (kMore) {
-            part = p.slots + (((size_t)b * p.hq + (size_t)h * G) * p.slots_per_row + p.others + split) * (kDim + 2);
-            part_stride = p.slots_per_row * (kDim + 2);
+            part = p.slots + (((size_t)b * p.hq + (size_t)h * G) * p.slots_per_row + p.others + split) * slot_floats(kDim);
+            part_stride = p.slots_per_row * slot_floats(kDim);
             part_max = kDim;
         } else {
             part = p.out + ((size_t)head * p.splits + split) * G * kStride;
@@ -297,7 +333,7 @@ attend_tc_kernel(Args p, const __grid_constant__ CUtensorMap map_k, const __grid
         else *to = v;
     };
     bool merges = p.splits > 1;              // the result is merged with those of other blocks, or other kernels
-    if constexpr (kMore) merges = merges || p.others > 0;
+    if constexpr (kMore) merges = merges || p.others > 0 || p.separate;
 
     if (T <= 0) {       // no cached row falls into this split (uniform for the block)
         if (kForm == kEarly) {                           // what is under way lands before the block's memory is given up
@@ -310,7 +346,7 @@ attend_tc_kernel(Args p, const __grid_constant__ CUtensorMap map_k, const __grid
         if (!merges) {
             for (int x = threadIdx.x; x < G * kDim; x += kTcThreads) put(out + x, 0.f);
         } else {
-            if (!kMore && kFp8 && p.separate) {          // (what the merge kernel multiplies by 0 must not be NaN)
+            if (!kMore && kSeparate && p.separate) {          // (what the merge kernel multiplies by 0 must not be NaN)
                 for (int x = threadIdx.x; x < G * kStride; x += kTcThreads) part[x] = 0.f;
                 __syncthreads();
             }
@@ -326,9 +362,13 @@ attend_tc_kernel(Args p, const __grid_constant__ CUtensorMap map_k, const __grid
             if (kForm != kEarly) fetch_queries();
             for (int i = kForm == kEarly && !kMore ? 1 : 0; i < 2 * T; ++i) {
                 bool value;
-                const int y = tile_y(t0 + source(i, &value));
+                const int t = t0 + source(i, &value), y = tile_y(t);
                 if (!mbar_wait(bar(kEmpty + i % kRing), ((i / kRing) & 1) ^ 1, abort_flag, sink)) break;
-                fetch_tile(value ? &map_v : &map_k, i, y);
+                const CUtensorMap *map = value ? &maps.v : &maps.k;
+                if constexpr (kMore) {
+                    if (t < prefix_tiles) map = value ? &maps.prefix_v : &maps.prefix_k;
+                }
+                fetch_tile(map, i, y);
             }
         }
         __syncwarp();
@@ -540,7 +580,7 @@ attend_tc_kernel(Args p, const __grid_constant__ CUtensorMap map_k, const __grid
     }
 
     // ---- merge the splits: out = sum_s 2^(m_s - m) num_s / sum_s 2^(m_s - m) l_s, block r of the cluster taking its share
-    if (merges && !(kFp8 && p.separate)) {
+    if (merges && !(kSeparate && p.separate)) {
         __syncwarp();
         if constexpr (kMore) {
             if (p.late) pdl_wait();         // the other kernel's slots
@@ -572,21 +612,39 @@ attend_tc_kernel(Args p, const __grid_constant__ CUtensorMap map_k, const __grid
                 den = fmaf(w, kForm == kEarly ? ls[s] : ld_cluster(row + (kHeadDim + 1) * 4u, s), den);
             }
             if constexpr (kMore) {
-                const float *other = p.slots + (((size_t)b * p.hq + (size_t)h * G + g) * p.slots_per_row) * (kDim + 2);
-                for (int s = 0; s < p.others; ++s, other += kDim + 2) {
-                    const float mo = other[kDim];
-                    if (mo == -INFINITY) continue;
-                    const float top = fmaxf(m, mo), wo = exp2f(mo - top), wm = exp2f(m - top);
-                    num = fmaf(wo, other[c], num * wm);
-                    den = fmaf(wo, other[kDim + 1], den * wm);
-                    m = top;
+                // the other kernel's slots, the loads of eight under way at a time
+                const float *other = p.slots + (((size_t)b * p.hq + (size_t)h * G + g) * p.slots_per_row) * slot_floats(kDim);
+                constexpr int kAhead = 8;
+                for (int s0 = 0; s0 < p.others; s0 += kAhead) {
+                    float mo[kAhead], lo[kAhead], no[kAhead], top = m;
+#pragma unroll
+                    for (int i = 0; i < kAhead; ++i) {
+                        mo[i] = -INFINITY;
+                        if (s0 + i < p.others) {
+                            const float *slot = other + (s0 + i) * slot_floats(kDim);
+                            mo[i] = slot[kDim], lo[i] = slot[kDim + 1], no[i] = slot[c];
+                        }
+                        top = fmaxf(top, mo[i]);
+                    }
+                    if (top == -INFINITY) continue;
+                    const float old = exp2f(m - top);
+                    num *= old, den *= old, m = top;
+#pragma unroll
+                    for (int i = 0; i < kAhead; ++i) {
+                        if (mo[i] == -INFINITY) continue;
+                        const float w = exp2f(mo[i] - m);
+                        num = fmaf(w, no[i], num);
+                        den = fmaf(w, lo[i], den);
+                    }
                 }
             }
             put(out + x, den > 0.f ? num / den : 0.f);
         }
         cluster_sync();                     // nobody leaves while its partial result is still being read
     } else if constexpr (kMore) {
-        if (p.late) pdl_wait();             // (who waits for this kernel's end has waited for the other's too)
+        // The merge kernel waits for this kernel's end, which is to be behind the other kernel's: the last block waits.  (Not all: a block that
+        // waits keeps the next one out.)
+        if (p.late && blockIdx.x == gridDim.x - 1) pdl_wait();
     }
 
     // ---------------------------------------------------------------------- common exit
@@ -600,59 +658,59 @@ attend_tc_kernel(Args p, const __grid_constant__ CUtensorMap map_k, const __grid
 }
 
 template <int G, int kSrc, int kForm, class Args>
-cudaError_t launch_tc_one(const Args &p, int heads, const CUtensorMap &mk, const CUtensorMap &mv, const CUtensorMap &mq,
-                          int dev, cudaStream_t s)
+cudaError_t launch_tc_one(const Args &p, int heads, const MapsFor<Args> &maps, int dev, cudaStream_t s)
 {
     static PerDevice done;
     const cudaError_t e = allow_smem_once(done, dev, attend_tc_kernel<G, kSrc, kForm, Args>, kTcSmem, true);
     if (e != cudaSuccess) return e;
     return launch_early(attend_tc_kernel<G, kSrc, kForm, Args>, (unsigned)(heads * p.splits), kTcThreads, kTcSmem, s,
-                        p.separate ? 1u : (unsigned)p.splits, p, mk, mv, mq);
+                        p.separate ? 1u : (unsigned)p.splits, p, maps);
 }
 template <int G, int kSrc, class Args>
-cudaError_t launch_tc_form(const Args &p, int heads, const CUtensorMap &mk, const CUtensorMap &mv, const CUtensorMap &mq, cudaStream_t s)
+cudaError_t launch_tc_form(const Args &p, int heads, const MapsFor<Args> &maps, cudaStream_t s)
 {
     int dev = 0, sms = 0;
     const cudaError_t e = device_sms(&dev, &sms);
     if (e != cudaSuccess) return e;
-    if (p.tiles_per_split > kTcMaxTiles) return launch_tc_one<G, kSrc, kTwo, Args>(p, heads, mk, mv, mq, dev, s);
+    if (p.tiles_per_split > kTcMaxTiles) return launch_tc_one<G, kSrc, kTwo, Args>(p, heads, maps, dev, s);
     // A block per SM, or two of few tiles: beside a second block of many an idle one's tile costs more than an early start gives (32 heads of 9
     // tiles, 288 blocks of one: 13.0 us, 12.1 early; 256 blocks of nine, 256 heads of which half are empty: 12.6, 13.2; 128 heads of 17 tiles, 1000
     // tokens: 15.6, 16.0).
     const long long blocks = (long long)heads * p.splits;
-    return blocks <= sms || (blocks <= 2ll * sms && p.tiles_per_split <= 4) ? launch_tc_one<G, kSrc, kEarly, Args>(p, heads, mk, mv, mq, dev, s)
-                                                                            : launch_tc_one<G, kSrc, kPlain, Args>(p, heads, mk, mv, mq, dev, s);
+    return blocks <= sms || (blocks <= 2ll * sms && p.tiles_per_split <= 4) ? launch_tc_one<G, kSrc, kEarly, Args>(p, heads, maps, dev, s)
+                                                                            : launch_tc_one<G, kSrc, kPlain, Args>(p, heads, maps, dev, s);
 }
 template <int G, class Args>
-cudaError_t launch_tc_for(const Args &p, int heads, int src, const CUtensorMap &mk, const CUtensorMap &mv, const CUtensorMap &mq,
-                          cudaStream_t s)
+cudaError_t launch_tc_for(const Args &p, int heads, int src, const MapsFor<Args> &maps, cudaStream_t s)
 {
-    return src == 1 ? launch_tc_form<G, 1, Args>(p, heads, mk, mv, mq, s) : src == 2 ? launch_tc_form<G, 2, Args>(p, heads, mk, mv, mq, s)
-                                                                           : launch_tc_form<G, 0, Args>(p, heads, mk, mv, mq, s);
+    return src == 1 ? launch_tc_form<G, 1, Args>(p, heads, maps, s) : src == 2 ? launch_tc_form<G, 2, Args>(p, heads, maps, s)
+                                                                           : launch_tc_form<G, 0, Args>(p, heads, maps, s);
 }
 
 
-// The tensor maps, and the instance for the group.  src: 0 = bf16 caches of 128 dimensions, 1 = E4M3 codes of 128 dimensions, 2 = bf16 caches
-// of 64 dimensions
+// src: 0 = bf16 caches of 128 dimensions, 1 = E4M3 codes of 128 dimensions, 2 = bf16 caches of 64 dimensions
+inline bool make_cache_map(CUtensorMap *map, const void *base, uint64_t rows, int src)
+{
+    return src != 0 ? sm100::make_map_row128(map, base, rows, src == 1) : sm100::make_map(map, base, rows, kTile);
+}
+// The tensor maps of the caches and the queries, and the instance for the group.
 template <class Args>
-cudaError_t launch_tc_group(const Args &p, const void *k_cache, const void *v_cache, const void *q_new, int batch, long long pool_pages, int src,
-                            cudaStream_t s)
+cudaError_t launch_tc_group(const Args &p, MapsFor<Args> maps, const void *k_cache, const void *v_cache, const void *q_new, int batch,
+                            long long pool_pages, int src, cudaStream_t s)
 {
     const uint64_t rows = p.block_table ? (uint64_t)pool_pages * kTile : (uint64_t)batch * p.hkv * p.cap;
-    CUtensorMap mk, mv, mq;
-    const bool maps_ok = src != 0 ? (sm100::make_map_row128(&mk, k_cache, rows, src == 1) && sm100::make_map_row128(&mv, v_cache, rows, src == 1))
-                                  : (sm100::make_map(&mk, k_cache, rows, kTile) && sm100::make_map(&mv, v_cache, rows, kTile));
-    const bool q_ok = src == 2 ? sm100::make_map_rows(&mq, q_new, (uint64_t)batch * p.hq, 64, 16) : sm100::make_map(&mq, q_new, (uint64_t)batch * p.hq, 16);
+    const bool maps_ok = make_cache_map(&maps.k, k_cache, rows, src) && make_cache_map(&maps.v, v_cache, rows, src);
+    const bool q_ok = src == 2 ? sm100::make_map_rows(&maps.q, q_new, (uint64_t)batch * p.hq, 64, 16) : sm100::make_map(&maps.q, q_new, (uint64_t)batch * p.hq, 16);
     if (!maps_ok || !q_ok) return cudaErrorInvalidValue;
     switch (p.hq / p.hkv) {
-        case 1: return launch_tc_for<1>(p, batch * p.hkv, src, mk, mv, mq, s);
-        case 2: return launch_tc_for<2>(p, batch * p.hkv, src, mk, mv, mq, s);
-        case 3: return launch_tc_for<3>(p, batch * p.hkv, src, mk, mv, mq, s);
-        case 4: return launch_tc_for<4>(p, batch * p.hkv, src, mk, mv, mq, s);
-        case 5: return launch_tc_for<5>(p, batch * p.hkv, src, mk, mv, mq, s);
-        case 6: return launch_tc_for<6>(p, batch * p.hkv, src, mk, mv, mq, s);
-        case 7: return launch_tc_for<7>(p, batch * p.hkv, src, mk, mv, mq, s);
-        case 8: return launch_tc_for<8>(p, batch * p.hkv, src, mk, mv, mq, s);
+        case 1: return launch_tc_for<1>(p, batch * p.hkv, src, maps, s);
+        case 2: return launch_tc_for<2>(p, batch * p.hkv, src, maps, s);
+        case 3: return launch_tc_for<3>(p, batch * p.hkv, src, maps, s);
+        case 4: return launch_tc_for<4>(p, batch * p.hkv, src, maps, s);
+        case 5: return launch_tc_for<5>(p, batch * p.hkv, src, maps, s);
+        case 6: return launch_tc_for<6>(p, batch * p.hkv, src, maps, s);
+        case 7: return launch_tc_for<7>(p, batch * p.hkv, src, maps, s);
+        case 8: return launch_tc_for<8>(p, batch * p.hkv, src, maps, s);
         default: return cudaErrorInvalidValue;
     }
 }

@@ -1,16 +1,16 @@
 // Attention of many query rows over a cache, CUDA-core form (fp32 products), and the merge of partial results.
 //
-// A block takes 64 query rows of one (problem, KV head) and goes once over its share of the key tiles, 64 keys at a time, with the running
-// maximum and sum of the softmax; the weighted sum stays in registers.  256 threads as 16 x 16: a thread owns 4 x 4 scores, then 4 rows x
-// d / 16 columns of the output; the 16 threads that share rows are half a warp, so that the weights change hands within the warp.
-// Bound by fp32 FMAs and the shared-memory reads that feed them (8 vectors per 64 FMAs of the scores).
+// A block takes 64 query rows (16 where a problem has no more) of one (problem, KV head) and goes once over its share of the key tiles, 64 keys
+// at a time, with the running maximum and sum of the softmax; the weighted sum stays in registers.  256 threads as 16 x 16: a thread owns
+// 4 x 4 scores (1 x 4), then 4 rows (1) x d / 16 columns of the output; the 16 threads that share rows are half a warp, so that the weights
+// change hands within the warp.  Bound by fp32 FMAs and the shared-memory reads that feed them (8 vectors per 64 FMAs of the scores; 5 per 16).
 #include "rkv_tokens.cuh"
 
 namespace rkv {
 
 namespace {
 
-constexpr int kRows = 64, kKeys = 64, kThreads = 256;
+constexpr int kKeys = 64, kThreads = 256;
 constexpr float kLog2e = 1.4426950408889634f;
 
 template <typename T> __device__ __forceinline__ float4 load4(const T *p);
@@ -32,13 +32,23 @@ template <> __device__ __forceinline__ float4 load4<uint8_t>(const uint8_t *p)  
 __device__ __forceinline__ void put(float *p, float v) { *p = v; }
 __device__ __forceinline__ void put(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
 
-template <int kDim> constexpr int rows_simt_smem() { return (2 * kRows * (kDim + 4) + kKeys * kDim + kRows * (kKeys + 4)) * 4; }
-
-template <typename TQ, typename TC, int kDim>
-__global__ void __launch_bounds__(kThreads) rows_simt_kernel(RowsParams p, int row_tiles)
+__device__ __forceinline__ void store4(float *p, float4 v) { *reinterpret_cast<float4 *>(p) = v; }
+__device__ __forceinline__ void store4(__nv_bfloat16 *p, float4 v)
 {
-    constexpr int kStride = kDim + 4, kPStride = kKeys + 4, kVecs = kDim / 4, kCols = kDim / 64;
-    static_assert(kRows == kKeys, "one strip of rows after the other");
+    const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
+    *reinterpret_cast<uint2 *>(p) = make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
+}
+
+template <int kDim, int kPer> constexpr int rows_simt_smem()
+{
+    return ((16 * kPer + kKeys) * (kDim + 4) + kKeys * kDim + 16 * kPer * (kKeys + 4)) * 4;
+}
+
+// kPer: rows of a thread
+template <typename TQ, typename TC, int kDim, int kPer>
+__global__ void __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) rows_simt_kernel(RowsParams p, int row_tiles)
+{
+    constexpr int kRows = 16 * kPer, kStride = kDim + 4, kPStride = kKeys + 4, kVecs = kDim / 4, kCols = kDim / 64;
     extern __shared__ float rows_smem[];
     float *sq = rows_smem, *sk = sq + kRows * kStride, *sv = sk + kKeys * kStride, *sp = sv + kKeys * kDim;
     pdl_wait();
@@ -77,61 +87,74 @@ __global__ void __launch_bounds__(kThreads) rows_simt_kernel(RowsParams p, int r
     }
 
     // of this thread's rows: the last and the first cached row that each sees
-    int last[4], from[4];
+    int last[kPer], from[kPer];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int at = len - n + (r0 + ty * 4 + i) / p.group;
+    for (int i = 0; i < kPer; ++i) {
+        const int at = len - n + (r0 + ty * kPer + i) / p.group;
         last[i] = p.causal ? at : len - 1;
         from[i] = p.causal && p.window > 0 ? at + 1 - p.window : 0;
     }
     const float scale = kLog2e * rsqrtf((float)kDim);
-    float m[4], l[4], o[4][kDim / 16];
+    float m[kPer], l[kPer], o[kPer][kDim / 16];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < kPer; ++i) {
         m[i] = -INFINITY, l[i] = 0.f;
 #pragma unroll
         for (int c = 0; c < kDim / 16; ++c) o[i][c] = 0.f;
     }
     const TC *kc = static_cast<const TC *>(p.k), *vc = static_cast<const TC *>(p.v);
     const int head = b * p.hkv + h;
-    for (int step = 2 * i0; step < 2 * i1; ++step) {             // half a tile of 128 keys at a time
+    // half a tile of 128 keys at a time; with one row to a thread there are registers to have the next half under way meanwhile
+    constexpr int kLoads = kKeys * kVecs / kThreads;
+    constexpr bool kAhead = kPer == 1;
+    float4 next_k[kLoads], next_v[kLoads];
+    auto fetch = [&](int step) {
         const int t = keys.tile(step >> 1), j0 = t * kTile + (step & 1) * kKeys;
-        if (j0 >= keys.hi) continue;
         const long long tile_start = rows_tile_start(p, head, t), start = tile_start + (step & 1) * kKeys;
-        const bool missing = tile_start < 0;
-        if (missing && threadIdx.x == 0) report(p.status, RKV_ERR_INVALID_ARG);
-        __syncthreads();                                         // the tiles of the step before have been read
-        for (int v = threadIdx.x; v < kKeys * kVecs; v += kThreads) {
-            const int r = v / kVecs, c = v % kVecs * 4;
-            float4 a = make_float4(0.f, 0.f, 0.f, 0.f), e = a;
-            if (!missing && keys.wanted(j0 + r)) {
-                a = load4<TC>(kc + (start + r) * kDim + c);
-                e = load4<TC>(vc + (start + r) * kDim + c);
+        if (tile_start < 0 && threadIdx.x == 0) report(p.status, RKV_ERR_INVALID_ARG);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int v = i * kThreads + threadIdx.x, r = v / kVecs, c = v % kVecs * 4;
+            next_k[i] = next_v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (tile_start >= 0 && keys.wanted(j0 + r)) {
+                next_k[i] = load4<TC>(kc + (start + r) * kDim + c);
+                next_v[i] = load4<TC>(vc + (start + r) * kDim + c);
             }
-            *reinterpret_cast<float4 *>(sk + r * kStride + c) = a;
-            *reinterpret_cast<float4 *>(sv + r * kDim + c) = e;
+        }
+    };
+    if (kAhead && i0 < i1) fetch(2 * i0);
+    for (int step = 2 * i0; step < 2 * i1; ++step) {
+        const int j0 = keys.tile(step >> 1) * kTile + (step & 1) * kKeys;
+        if (!kAhead) fetch(step);
+        __syncthreads();                                         // the tiles of the step before have been read
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int v = i * kThreads + threadIdx.x, r = v / kVecs, c = v % kVecs * 4;
+            *reinterpret_cast<float4 *>(sk + r * kStride + c) = next_k[i];
+            *reinterpret_cast<float4 *>(sv + r * kDim + c) = next_v[i];
         }
         __syncthreads();
-        float s[4][4];
+        if (kAhead && step + 1 < 2 * i1) fetch(step + 1);
+        float s[kPer][4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < kPer; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
 #pragma unroll 4
         for (int c = 0; c < kDim; c += 4) {
-            float4 a[4], e[4];
+            float4 a[kPer], e[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) a[i] = *reinterpret_cast<const float4 *>(sq + (ty * 4 + i) * kStride + c);
+            for (int i = 0; i < kPer; ++i) a[i] = *reinterpret_cast<const float4 *>(sq + (ty * kPer + i) * kStride + c);
 #pragma unroll
             for (int j = 0; j < 4; ++j) e[j] = *reinterpret_cast<const float4 *>(sk + (tx + 16 * j) * kStride + c);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < kPer; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
                     s[i][j] = fmaf(a[i].x, e[j].x, fmaf(a[i].y, e[j].y, fmaf(a[i].z, e[j].z, fmaf(a[i].w, e[j].w, s[i][j]))));
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < kPer; ++i) {
             float top = m[i];
             bool sees[4];
 #pragma unroll
@@ -151,7 +174,7 @@ __global__ void __launch_bounds__(kThreads) rows_simt_kernel(RowsParams p, int r
             for (int j = 0; j < 4; ++j) {
                 const float w = sees[j] ? exp2f(s[i][j] - base) : 0.f;
                 sum += w;
-                sp[(ty * 4 + i) * kPStride + tx + 16 * j] = w;
+                sp[(ty * kPer + i) * kPStride + tx + 16 * j] = w;
             }
             l[i] = l[i] * shrink + sum;                          // (of this thread's keys; added up at the end)
 #pragma unroll
@@ -160,16 +183,16 @@ __global__ void __launch_bounds__(kThreads) rows_simt_kernel(RowsParams p, int r
         __syncwarp();
 #pragma unroll 4
         for (int k = 0; k < kKeys; k += 4) {
-            float4 w[4];
+            float4 w[kPer];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = *reinterpret_cast<const float4 *>(sp + (ty * 4 + i) * kPStride + k);
+            for (int i = 0; i < kPer; ++i) w[i] = *reinterpret_cast<const float4 *>(sp + (ty * kPer + i) * kPStride + k);
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk)
 #pragma unroll
                 for (int c = 0; c < kCols; ++c) {
                     const float4 e = *reinterpret_cast<const float4 *>(sv + (k + kk) * kDim + c * 64 + tx * 4);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
+                    for (int i = 0; i < kPer; ++i) {
                         const float f = kk == 0 ? w[i].x : kk == 1 ? w[i].y : kk == 2 ? w[i].z : w[i].w;
                         o[i][4 * c] = fmaf(f, e.x, o[i][4 * c]), o[i][4 * c + 1] = fmaf(f, e.y, o[i][4 * c + 1]);
                         o[i][4 * c + 2] = fmaf(f, e.z, o[i][4 * c + 2]), o[i][4 * c + 3] = fmaf(f, e.w, o[i][4 * c + 3]);
@@ -179,14 +202,14 @@ __global__ void __launch_bounds__(kThreads) rows_simt_kernel(RowsParams p, int r
         __syncwarp();
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < kPer; ++i) {
 #pragma unroll
         for (int off = 8; off > 0; off >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], off);
-        const int r = ty * 4 + i;
+        const int r = ty * kPer + i;
         if (r >= rows) continue;
         const int t = first + (r0 + r) / p.group, qh = h * p.group + (r0 + r) % p.group;
         if (p.part) {
-            float *dst = p.part + (((size_t)t * p.hq + qh) * p.slots + p.slot + split) * (kDim + 2);
+            float *dst = p.part + (((size_t)t * p.hq + qh) * p.slots + p.slot + split) * slot_floats(kDim);
 #pragma unroll
             for (int c = 0; c < kDim / 16; ++c) dst[(c >> 2) * 64 + tx * 4 + (c & 3)] = o[i][c];
             if (tx == 0) dst[kDim] = m[i], dst[kDim + 1] = l[i];
@@ -198,13 +221,18 @@ __global__ void __launch_bounds__(kThreads) rows_simt_kernel(RowsParams p, int r
     }
 }
 
-// out = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s over a row's slots, in fixed order; a block per query token, the heads one after the other
+// out = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s over a row's slots, in fixed order; a warp per row.  The loads of eight slots are under way
+// at a time (one after the other they took a memory latency each).
+constexpr int kMergeWarps = 4, kMergeAhead = 8;
 template <typename TQ>
-__global__ void __launch_bounds__(128) rows_merge_kernel(RowsParams p)
+__global__ void __launch_bounds__(kMergeWarps * 32) rows_merge_kernel(RowsParams p)
 {
     pdl_trigger();
     pdl_wait();
-    const int t = blockIdx.x / p.hq, qh = blockIdx.x % p.hq;
+    const int lane = threadIdx.x & 31;
+    const long long row = (long long)blockIdx.x * kMergeWarps + (threadIdx.x >> 5);
+    if (row >= (long long)p.tokens.total * p.hq) return;
+    const int t = (int)(row / p.hq), qh = (int)(row % p.hq);
     if (p.tokens.offsets) {                                      // rows of no sequence stay as they are
         int first = 0, lo = 0, hi = p.tokens.count;              // the last sequence that starts at or before t
         while (hi - lo > 1) {
@@ -214,42 +242,69 @@ __global__ void __launch_bounds__(128) rows_merge_kernel(RowsParams p)
         const int n = token_span(p.tokens, lo, &first);
         if (t < first || t >= first + n) return;
     }
-    const float *part = p.part + ((size_t)t * p.hq + qh) * p.slots * (p.d + 2);
-    float m = -INFINITY;
-    for (int s = 0; s < p.slots; ++s) m = fmaxf(m, part[s * (p.d + 2) + p.d]);
-    for (int c = threadIdx.x; c < p.d; c += 128) {
-        float num = 0.f, den = 0.f;
-        for (int s = 0; s < p.slots; ++s) {
-            const float *x = part + s * (p.d + 2);
-            if (x[p.d] == -INFINITY) continue;                   // a share without a visible key
-            const float w = exp2f(x[p.d] - m);
-            num = fmaf(w, x[c], num);
-            den = fmaf(w, x[p.d + 1], den);
+    const int stride = slot_floats(p.d);
+    const float *part = p.part + (size_t)row * p.slots * stride;
+    for (int c = lane * 4; c < p.d; c += 128) {
+        float m = -INFINITY, den = 0.f;
+        float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int s0 = 0; s0 < p.slots; s0 += kMergeAhead) {
+            float4 o[kMergeAhead];
+            float2 ml[kMergeAhead];
+            float top = m;
+#pragma unroll
+            for (int i = 0; i < kMergeAhead; ++i) {
+                ml[i] = make_float2(-INFINITY, 0.f);
+                if (s0 + i < p.slots) {
+                    o[i] = *reinterpret_cast<const float4 *>(part + (s0 + i) * stride + c);
+                    ml[i] = *reinterpret_cast<const float2 *>(part + (s0 + i) * stride + p.d);
+                }
+                top = fmaxf(top, ml[i].x);
+            }
+            if (top == -INFINITY) continue;                      // no visible key so far
+            const float old = exp2f(m - top);
+            den *= old, num.x *= old, num.y *= old, num.z *= old, num.w *= old;
+            m = top;
+#pragma unroll
+            for (int i = 0; i < kMergeAhead; ++i) {
+                if (ml[i].x == -INFINITY) continue;              // a share without a visible key
+                const float w = exp2f(ml[i].x - m);
+                den = fmaf(w, ml[i].y, den);
+                num.x = fmaf(w, o[i].x, num.x), num.y = fmaf(w, o[i].y, num.y), num.z = fmaf(w, o[i].z, num.z), num.w = fmaf(w, o[i].w, num.w);
+            }
         }
-        put(static_cast<TQ *>(p.out) + t * p.out_stride + (size_t)qh * p.d + c, den == 0.f ? 0.f : num / den);
+        const float inv = den == 0.f ? 0.f : 1.f / den;
+        store4(static_cast<TQ *>(p.out) + t * p.out_stride + (size_t)qh * p.d + c, make_float4(num.x * inv, num.y * inv, num.z * inv, num.w * inv));
     }
 }
 
-template <typename TQ, typename TC, int kDim>
+template <typename TQ, typename TC, int kDim, int kPer>
 cudaError_t launch_simt_for(const RowsParams &p, cudaStream_t s)
 {
     static PerDevice done;
     int dev = 0, sms = 0;
     cudaError_t e = device_sms(&dev, &sms);
     if (e != cudaSuccess) return e;
-    if ((e = allow_smem_once(done, dev, rows_simt_kernel<TQ, TC, kDim>, rows_simt_smem<kDim>())) != cudaSuccess) return e;
-    const long long row_tiles = ((long long)p.tokens.longest * p.group + kRows - 1) / kRows;
+    if ((e = allow_smem_once(done, dev, rows_simt_kernel<TQ, TC, kDim, kPer>, rows_simt_smem<kDim, kPer>())) != cudaSuccess) return e;
+    const long long row_tiles = ((long long)p.tokens.longest * p.group + 16 * kPer - 1) / (16 * kPer);
     const long long blocks = row_tiles * p.hkv * p.tokens.count * p.splits;
     if (blocks > 0x7fffffffll) return cudaErrorInvalidValue;
-    return launch_early(rows_simt_kernel<TQ, TC, kDim>, (unsigned)blocks, kThreads, rows_simt_smem<kDim>(), s, 1, p, (int)row_tiles);
+    return launch_early(rows_simt_kernel<TQ, TC, kDim, kPer>, (unsigned)blocks, kThreads, rows_simt_smem<kDim, kPer>(), s, 1, p, (int)row_tiles);
+}
+template <typename TQ, typename TC, int kDim>
+cudaError_t launch_simt_dim(const RowsParams &p, cudaStream_t s)
+{
+    return rows_simt_rows(p) == 16 ? launch_simt_for<TQ, TC, kDim, 1>(p, s) : launch_simt_for<TQ, TC, kDim, 4>(p, s);
 }
 template <typename TQ, typename TC>
 cudaError_t launch_simt_type(const RowsParams &p, cudaStream_t s)
 {
-    return p.d == 64 ? launch_simt_for<TQ, TC, 64>(p, s) : p.d == 128 ? launch_simt_for<TQ, TC, 128>(p, s) : launch_simt_for<TQ, TC, 256>(p, s);
+    return p.d == 64 ? launch_simt_dim<TQ, TC, 64>(p, s) : p.d == 128 ? launch_simt_dim<TQ, TC, 128>(p, s) : launch_simt_dim<TQ, TC, 256>(p, s);
 }
 
 }  // namespace
+
+// Query rows of a block.
+int rows_simt_rows(const RowsParams &p) { return (long long)p.tokens.longest * p.group <= 16 ? 16 : 64; }
 
 cudaError_t launch_rows_simt(const RowsParams &p, int dtype, cudaStream_t s)
 {
@@ -259,8 +314,9 @@ cudaError_t launch_rows_simt(const RowsParams &p, int dtype, cudaStream_t s)
 
 cudaError_t launch_rows_merge(const RowsParams &p, int dtype, cudaStream_t s)
 {
-    const unsigned blocks = (unsigned)p.tokens.total * (unsigned)p.hq;
-    return launch_early(dtype == RKV_F32 ? rows_merge_kernel<float> : rows_merge_kernel<__nv_bfloat16>, blocks, 128, 0, s, 1, p);
+    const long long blocks = ((long long)p.tokens.total * p.hq + kMergeWarps - 1) / kMergeWarps;
+    if (blocks > 0x7fffffffll) return cudaErrorInvalidValue;
+    return launch_early(dtype == RKV_F32 ? rows_merge_kernel<float> : rows_merge_kernel<__nv_bfloat16>, (unsigned)blocks, kMergeWarps * 32, 0, s, 1, p);
 }
 
 }  // namespace rkv

@@ -519,7 +519,7 @@ rows_tc_kernel(RowsParams p, int tokens_per_tile, int pieces, int items, const _
             const int t = x.t0 + r * tokens_per_tile + row / p.group, qh = x.h * p.group + row % p.group, c0 = half * (kDim / 2);
             const bool mine = row < tokens_per_tile * p.group && t <= x.t1;  // else: nobody's row, computed and dropped
             const float inv = l == 0.f ? 0.f : 1.f / l;
-            float *part = p.part ? p.part + (((size_t)(x.first + t) * p.hq + qh) * p.slots + p.slot + x.split) * (kDim + 2) : nullptr;
+            float *part = p.part ? p.part + (((size_t)(x.first + t) * p.hq + qh) * p.slots + p.slot + x.split) * slot_floats(kDim) : nullptr;
             __nv_bfloat16 *out = p.part ? nullptr : static_cast<__nv_bfloat16 *>(p.out) + (x.first + t) * p.out_stride + (size_t)qh * kDim;
 #pragma unroll 1
             for (int c = 0; c < kDim / 2; c += 32) {
@@ -538,7 +538,7 @@ rows_tc_kernel(RowsParams p, int tokens_per_tile, int pieces, int items, const _
                 if (part) {
                     if (mine)
 #pragma unroll
-                        for (int e = 0; e < 32; e += 2) *reinterpret_cast<uint2 *>(part + c0 + c + e) = make_uint2(o[e], o[e + 1]);
+                        for (int e = 0; e < 32; e += 4) *reinterpret_cast<uint4 *>(part + c0 + c + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
                     continue;
                 }
                 // Four lanes exchange the vectors of their rows, so that a store writes 64 bytes of eight rows, not 16 of 32: the rows lie far apart,

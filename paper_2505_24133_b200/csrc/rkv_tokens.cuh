@@ -56,11 +56,12 @@ struct RowsParams {
     int causal, window, sinks;      // causal: token t of n stands in row len - n + t and sees rows up to its own; else every token sees all rows
     int compact_tiles;              // > 0: k and v are [count][hkv][compact_tiles][128][d], the tiles that the call sees (CallTiles), in turn
     int splits, slot, slots;        // blocks that share a row tile's keys; their partial results are slots slot .. of the rows' `slots`
-    float *part;                    // [total * hq][slots][d + 2]: weighted sum, maximum (base 2), sum of weights; null: `out` is written
+    float *part;                    // [total * hq][slots][d + 4]: weighted sum, maximum (base 2), sum of weights; null: `out` is written
     void *out;
     int32_t *status;
     long long wait_cycles;
 };
+__host__ __device__ constexpr int slot_floats(int d) { return d + 4; }        // (whole 16-byte vectors)
 // The key tiles of 128 rows that tokens t0 .. t1 of a problem look at: the first `sink_tiles`, then those from `first` on.
 struct KeyTiles {
     int sink_tiles, first, count;
@@ -101,6 +102,7 @@ __device__ __forceinline__ long long rows_tile_start(const RowsParams &p, int he
 }
 // 8-bit caches: the tiles that a call sees, as bf16, rows that it does not see as zeros; `wide` holds K's, then V's.  `p` becomes the call on them.
 cudaError_t launch_rows_widen(RowsParams *p, void *wide, int tiles, cudaStream_t s);
+int rows_simt_rows(const RowsParams &p);
 cudaError_t launch_rows_simt(const RowsParams &p, int dtype, cudaStream_t s);
 bool rows_sm100_supported(int dtype, int d, int group);
 int rows_sm100_tiles(const RowsParams &p);                  // row tiles of a block
@@ -109,8 +111,10 @@ cudaError_t launch_rows_sm100(const RowsParams &p, cudaStream_t s);
 // other kernels, and of the splits where they are blocks of their own (then the merge kernel follows); `late`: the kernel before this one
 // leaves those slots and lets this one in only when everything before itself is done.
 bool attend_more_supported(int dtype, int d, int group, long long tiles);
-void attend_more_plan(RowsParams *p, int dtype, long long tiles, int sms, bool *separate);
-cudaError_t launch_attend_more(const RowsParams &p, int dtype, long long tiles, bool separate, int others, bool late, cudaStream_t s);
+void attend_more_plan(RowsParams *p, int dtype, long long tiles, int sms, bool others, bool *separate);
+// `prefix`: prefixes that the kernel reads itself, in front of every sequence's own rows; null: none.
+cudaError_t launch_attend_more(const RowsParams &p, int dtype, long long tiles, bool separate, int others, bool late, const RowsParams *prefix,
+                               cudaStream_t s);
 cudaError_t launch_rows_merge(const RowsParams &p, int dtype, cudaStream_t s);
 
 }  // namespace rkv

@@ -119,7 +119,7 @@ def test_prefix_attention_refuses(rkv, case, want):
     d = _desc(rkv, workspace=0x10000, workspace_bytes=1 << 40)
     for k, v in case.get("desc", {}).items():
         setattr(d, k, v)
-    x = rkv.RkvPrefix(GOOD, GOOD, 2, 500, GOOD, None, 0)
+    x = rkv.RkvPrefix(GOOD, GOOD, 2, 100000, GOOD, None, 0)
     for k, v in case.get("prefix", {}).items():
         setattr(x, k, v)
     assert rkv.rkv_prefix_attention(d, a["k_cache"], a["v_cache"], a["q"], a["seq"], a["out"], a["budget"], a["buffer"], x, 0) == want
@@ -130,5 +130,5 @@ def test_workspace_sizes(rkv):
     d, t = _desc(rkv), _tokens(rkv)
     assert rkv.rkv_window_workspace_bytes(d, 1000, 1, t, -1, 0) == 0 and rkv.rkv_window_workspace_bytes(_desc(rkv, head_dim=32), 1000, 1, t, 0, 0) == 0
     assert rkv.rkv_window_workspace_bytes(_desc(rkv, batch=512), 1000, 1, rkv.rkv_tokens(512 * 64, 64), 0, 0) == 0
-    x = rkv.RkvPrefix(GOOD, GOOD, 2, 500, GOOD, None, 0)
+    x = rkv.RkvPrefix(GOOD, GOOD, 2, 100000, GOOD, None, 0)
     assert rkv.rkv_prefix_workspace_bytes(d, 1000, 1, x) > 0 and rkv.rkv_prefix_workspace_bytes(_desc(rkv, batch=3), 1000, 1, x) == 0
