@@ -23,7 +23,7 @@ void attend_more_plan(RowsParams *p, int dtype, long long tiles, int sms, bool o
     const int heads = p->tokens.count * p->hkv;
     p->splits = attend_tc_splits(heads, (int)tiles * kTile, sms);
     *separate = others && (long long)heads * p->splits > 2ll * sms;
-    *separate = *separate || p->splits > 1 && source_of(dtype, p->d) != 0 && (long long)heads * p->splits > 4ll * sms;
+    *separate = *separate || p->splits > 1 && source_of(dtype, p->d) == 2 && (long long)heads * p->splits > 4ll * sms;
 }
 
 cudaError_t launch_attend_more(const RowsParams &r, int dtype, long long tiles, bool separate, int others, bool late, const RowsParams *prefix,

@@ -34,6 +34,13 @@
 // (four raw stages and a single operand tile were measured slower: the chain widen -> product must not serialise); everything else is the same, at half the bytes per cached
 // row.  Rows beyond the length are written as zeros there.
 //
+// 8-bit caches, as they are stored (kCodes, the calls of AttendTcMore): with bf16 operands the chain widen -> product of a block bounds the
+// call at 4 TB/s, so here both products take the codes themselves (kind::f8f6f4; products of codes are exact, the accumulators fp32), and the other
+// operands come in two E4M3 parts each, hi and 16 times what hi left, in the rows g and 8 + g that the bf16 weights' two parts take.  A query row
+// is scaled by a power of two to a largest element in [128, 256): two parts of four bits hold a bf16 number exactly, elements below 2^-13 of
+// the largest to 2^-21 of it.  A weight times 256 is held to 2^-8 of itself, as one bf16 part would hold it (to 2^-22 in all where that
+// is more); the sum of the weights is taken from the parts.
+//
 // Every mbarrier wait is bounded; on expiry the block records RKV_ERR_TIMEOUT,
 // writes zeros and leaves through the common exit that frees TMEM.  No TMA multicast.
 #pragma once
@@ -62,11 +69,13 @@ constexpr uint32_t kTcTmemCols = 256;                // 16 (output) per chunk + 
 constexpr int kOffRing = 0;                          // bf16 caches: kTcStages tiles.  8-bit caches: kConvBufs widened tiles,
 constexpr int kConvBufs = 2;
 constexpr int kRawStages = 2;
+constexpr int kCodeStages = 6;                       // ring of tiles of codes as they are stored, in the room of kTcStages bf16 ones
 constexpr int kOffRaw = kConvBufs * kTcTileBytes;    // then kRawStages raw stages of 16 KB
 constexpr int kRawBytes = kTile * kHeadDim;          // a tile of E4M3 codes
 constexpr int kOffQ = kOffRing + kTcStages * kTcTileBytes;
 static_assert(kOffRaw + kRawStages * kRawBytes <= kOffQ, "the 8-bit layout fits the room of the ring");
 constexpr int kOffP = kOffQ + kTcSmall;              // two buffers
+constexpr int kOffCodeQ = kOffP + kTcSmall / 2;       // [16 x 128] codes: 2 KB each, the queries' parts behind the first buffer's weights
 constexpr int kOffRed = kOffP + 2 * kTcSmall;        // [4 warps][8] floats: reductions over the softmax threads
 constexpr int kOffBars = kOffRed + 4 * 8 * 4;
 enum {
@@ -79,7 +88,10 @@ enum {
     kBarOut = kBarPEmpty + 2,            // the output columns are final
     kBarRawFull,                                 // [kRawStages] 8-bit caches: codes landed
     kBarRawEmpty = kBarRawFull + kRawStages,     // [kRawStages] ... widened (128 softmax threads)
-    kTcNumBars = kBarRawEmpty + kRawStages
+    kBarCodeFull = kBarRawEmpty + kRawStages,    // [kCodeStages] codes as they are stored: tile landed
+    kBarCodeEmpty = kBarCodeFull + kCodeStages,  // [kCodeStages] ... read by the tensor cores
+    kBarCodeQ = kBarCodeEmpty + kCodeStages,     // the queries' parts are written (128 softmax threads)
+    kTcNumBars
 };
 constexpr int kOffMisc = kOffBars + kTcNumBars * 8;  // TMEM base, abort flag
 constexpr int kTcSmem = kOffMisc + 16 + 1024;        // + slack for the 1024-byte alignment
@@ -152,6 +164,28 @@ __device__ __forceinline__ uint32_t small_off(int g, int k)
     return (uint32_t)(half * (kTcSmall / 2) + g * 128 + ((((kk >> 3) ^ (g & 7)) << 4) | ((kk & 7) << 1)));
 }
 
+// The same for a [16 x 128] operand of codes: rows of 128 bytes.
+__device__ __forceinline__ uint32_t code_off(int g, int k) { return (uint32_t)(g * 128 + (((k >> 4) ^ (g & 7)) << 4) + (k & 15)); }
+// x as hi + lo / 16 in two codes
+__device__ __forceinline__ void two_codes(float x, uint8_t *hi, uint8_t *lo, float *value)
+{
+    const __nv_fp8_storage_t h = __nv_cvt_float_to_fp8(x, __NV_SATFINITE, __NV_E4M3);
+    const float hf = __half2float(__half(__nv_cvt_fp8_to_halfraw(h, __NV_E4M3)));
+    const __nv_fp8_storage_t l = __nv_cvt_float_to_fp8((x - hf) * 16.f, __NV_SATFINITE, __NV_E4M3);
+    *hi = h;
+    *lo = l;
+    *value = hf + __half2float(__half(__nv_cvt_fp8_to_halfraw(l, __NV_E4M3))) * 0.0625f;
+}
+__device__ __forceinline__ void umma_codes(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accum)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accum)
+        : "memory");
+}
+
 // With kFp8, kBarFull / kBarEmpty [0 .. kConvBufs) stand for the widened tiles (filled by the softmax threads, 128 arrivals).
 // kForm: instances of their own, since a block's time is a chain of latencies that code for the others' sake lengthens.
 //   kPlain  the length first, then what it says there is
@@ -161,14 +195,17 @@ __device__ __forceinline__ uint32_t small_off(int g, int k)
 //           (1024 heads of 9 tiles, three quarters of the sequences empty: 25.4 us, and 32.2 with the early tiles).
 //   kTwo    blocks of more tiles than one chunk takes
 // kSrc: 0 = bf16 caches of 128 dimensions (tiles go to the tensor cores as they land), 1 = E4M3 codes of 128 dimensions,
-// 2 = bf16 caches of 64 dimensions (both: rows of 128 bytes, widened / padded with zeros into bf16 operand tiles of
+// 3 = E4M3 codes of 128 dimensions as they are stored (AttendTcMore), 2 = bf16 caches of 64 dimensions (1 and 2: rows of 128 bytes, widened / padded with zeros into bf16 operand tiles of
 // 128 dimensions; the queries of the 64-dimension case fill the first half of their operand, the rest stays zero).
 enum { kPlain, kEarly, kTwo };
 template <int G, int kSrc, int kForm, class Args>
 __global__ void __launch_bounds__(kTcThreads, 2)
 attend_tc_kernel(Args p, const __grid_constant__ MapsFor<Args> maps)
 {
-    constexpr bool kFp8 = kSrc != 0;            // the tiles pass through the softmax threads on their way to the tensor cores
+    constexpr bool kFp8 = kSrc == 1 || kSrc == 2;            // the tiles pass through the softmax threads on their way to the tensor cores
+    constexpr bool kCodes = kSrc == 3;          // E4M3 codes as they are stored
+    constexpr int kStages = kCodes ? kCodeStages : kTcStages, kTileRoom = kCodes ? kRawBytes : kTcTileBytes;
+    constexpr int kRingFull = kCodes ? (int)kBarCodeFull : (int)kBarFull, kRingEmpty = kCodes ? (int)kBarCodeEmpty : (int)kBarEmpty;
     constexpr int kDim = kSrc == 2 ? 64 : kHeadDim;          // head dimension of the caches, the queries and the output
     constexpr bool kMore = std::is_same<Args, AttendTcMore>::value;
     constexpr bool kSeparate = kFp8 || kMore;   // the splits may be blocks of their own
@@ -194,6 +231,13 @@ attend_tc_kernel(Args p, const __grid_constant__ MapsFor<Args> maps)
         for (int s = 0; s < kRawStages; ++s) {
             mbar_init(bar(kBarRawFull + s), 1);
             mbar_init(bar(kBarRawEmpty + s), 128);
+        }
+        if (kCodes) {
+            for (int s = 0; s < kCodeStages; ++s) {
+                mbar_init(bar(kBarCodeFull + s), 1);
+                mbar_init(bar(kBarCodeEmpty + s), 1);
+            }
+            mbar_init(bar(kBarCodeQ), 128);
         }
         mbar_init(bar(kBarQ), 1);
         mbar_init(bar(kBarScores), 1);
@@ -257,6 +301,10 @@ attend_tc_kernel(Args p, const __grid_constant__ MapsFor<Args> maps)
             const int s = i % kRawStages;
             mbar_expect_tx(bar(kBarRawFull + s), kRawBytes);
             tma_load_2d(sbase + kOffRaw + s * kRawBytes, map, 0, y, bar(kBarRawFull + s));
+        } else if (kCodes) {
+            const int s = i % kCodeStages;
+            mbar_expect_tx(bar(kBarCodeFull + s), kRawBytes);
+            tma_load_2d(sbase + kOffRing + s * kRawBytes, map, 0, y, bar(kBarCodeFull + s));
         } else {
             const int s = i % kTcStages;
             const uint32_t dst = sbase + kOffRing + s * kTcTileBytes;
@@ -358,7 +406,7 @@ attend_tc_kernel(Args p, const __grid_constant__ MapsFor<Args> maps)
     } else if (warp == 4) {
         // ------------------------------------------------------------------ TMA producer
         if (lane == 0) {
-            constexpr int kRing = kFp8 ? kRawStages : kTcStages, kEmpty = kFp8 ? kBarRawEmpty : kBarEmpty;
+            constexpr int kRing = kFp8 ? kRawStages : kStages, kEmpty = kFp8 ? (int)kBarRawEmpty : kRingEmpty;
             if (kForm != kEarly) fetch_queries();
             for (int i = kForm == kEarly && !kMore ? 1 : 0; i < 2 * T; ++i) {
                 bool value;
@@ -375,9 +423,9 @@ attend_tc_kernel(Args p, const __grid_constant__ MapsFor<Args> maps)
     } else if (warp == 5) {
         // ------------------------------------------------------------------ MMA issuer
         if (lane == 0) {
-            bool ok = mbar_wait(bar(kBarQ), 0, abort_flag, sink);
-            const uint32_t idesc_s = instr_desc(kTile, 16);
-            constexpr int kBufs = kFp8 ? kConvBufs : kTcStages;      // operand tiles the tensor cores read from
+            bool ok = mbar_wait(bar(kCodes ? kBarCodeQ : kBarQ), 0, abort_flag, sink);
+            const uint32_t idesc_s = kCodes ? instr_desc_codes(kTile, 16) : instr_desc(kTile, 16);
+            constexpr int kBufs = kFp8 ? kConvBufs : kStages;        // operand tiles the tensor cores read from
             // f32 accumulate, bf16 x bf16, A MN-major (bit 15), B K-major, M = 128, N = 16
             const uint32_t idesc_o = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | ((16u >> 3) << 17) | ((128u >> 4) << 24);
             int i = 0;                                       // tiles of the ring so far
@@ -386,20 +434,35 @@ attend_tc_kernel(Args p, const __grid_constant__ MapsFor<Args> maps)
                 // (the second chunk's scores take the columns of the first's: the last of its weights have been waited for)
                 for (int t = 0; t < n && ok; ++t, ++i) {     // scores of key tile t into its own 16 columns
                     const int s = i % kBufs;
-                    ok = mbar_wait(bar(kBarFull + s), (i / kBufs) & 1, abort_flag, sink);
+                    ok = mbar_wait(bar(kRingFull + s), (i / kBufs) & 1, abort_flag, sink);
                     if (!ok) break;
                     tc_fence_after();
-                    umma_tile_k128_halves(tmem + 16 * (chunks + t), sbase + kOffRing + s * kTcTileBytes, kTcHalf, sbase + kOffQ,
+                    if (kCodes)
+                        umma_tile_row128<true>(tmem + 16 * (chunks + t), sbase + kOffRing + s * kRawBytes, sbase + kOffCodeQ, idesc_s);
+                    else
+                        umma_tile_k128_halves(tmem + 16 * (chunks + t), sbase + kOffRing + s * kTcTileBytes, kTcHalf, sbase + kOffQ,
                                           kTcSmall / 2, idesc_s);
-                    umma_commit(bar(kBarEmpty + s));
+                    umma_commit(bar(kRingEmpty + s));
                 }
                 if (ok) umma_commit(bar(kBarScores));
                 for (int t = 0; t < n && ok; ++t, ++i) {     // O^T += V_t^T . P_t
                     const int s = i % kBufs, pt = done + t, pb = pt & 1;
-                    ok = mbar_wait(bar(kBarFull + s), (i / kBufs) & 1, abort_flag, sink) &&
+                    ok = mbar_wait(bar(kRingFull + s), (i / kBufs) & 1, abort_flag, sink) &&
                          mbar_wait(bar(kBarPFull + pb), (pt >> 1) & 1, abort_flag, sink);
                     if (!ok) break;
                     tc_fence_after();
+                    if (kCodes) {
+#pragma unroll
+                        for (int ks = 0; ks < 4; ++ks) {     // 32 keys per step
+                            const uint32_t a_addr = sbase + kOffRing + s * kRawBytes + ks * 4096, b_addr = sbase + kOffP + pb * kTcSmall + ks * 32;
+                            // A: the 128 dimensions are one atom along M, 8-row groups along K 1 KB apart
+                            umma_codes(tmem + 16 * c, smem_desc(a_addr), smem_desc(b_addr), instr_desc_codes(kTile, 16) | (1u << 15),
+                                       (t > 0 || ks > 0) ? 1u : 0u);
+                        }
+                        umma_commit(bar(kRingEmpty + s));
+                        umma_commit(bar(kBarPEmpty + pb));
+                        continue;
+                    }
                     const uint32_t v_tile = sbase + kOffRing + s * kTcTileBytes, p_tile = sbase + kOffP + pb * kTcSmall;
 #pragma unroll
                     for (int ks = 0; ks < 8; ++ks) {         // 16 keys per step
@@ -410,7 +473,7 @@ attend_tc_kernel(Args p, const __grid_constant__ MapsFor<Args> maps)
                                             ((uint64_t)(1024u >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
                         umma(tmem + 16 * c, da, smem_desc(b_addr), idesc_o, (t > 0 || ks > 0) ? 1u : 0u);
                     }
-                    umma_commit(bar(kBarEmpty + s));
+                    umma_commit(bar(kRingEmpty + s));
                     umma_commit(bar(kBarPEmpty + pb));
                 }
             }
@@ -454,6 +517,41 @@ attend_tc_kernel(Args p, const __grid_constant__ MapsFor<Args> maps)
             return true;
         };
         bool ok = true;
+        float unscale[G];                            // kCodes: from the scaled query's scores back, in the base-2 domain
+        if constexpr (kCodes) {
+            // 16 threads to a query row, eight elements each: the row's scale, then its parts
+            ok = mbar_wait(bar(kBarQ), 0, abort_flag, sink);
+            float f[8], most = 0.f;
+            const int g = r >> 4, k0 = (r & 15) * 8;
+            Elem<__nv_bfloat16>::unpack(*reinterpret_cast<const uint4 *>(smem + kOffQ + small_off(g, k0)), f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(f[e]));
+#pragma unroll
+            for (int off = 8; off > 0; off >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, off));
+            // 2^(134 - exponent field) puts the largest into [128, 256); a row of zeros, or of numbers under 2^-100, by 2^100 at most
+            const int up = min(max(134 - (int)(__float_as_uint(most) >> 23), -100), 100);
+            const float scale = __uint_as_float((uint32_t)(127 + up) << 23);
+            if (g < G) {
+                uint8_t hi[8], lo[8];
+                float value;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) two_codes(f[e] * scale, hi + e, lo + e, &value);
+                *reinterpret_cast<uint2 *>(smem + kOffCodeQ + code_off(g, k0)) = make_uint2(hi[0] | hi[1] << 8 | hi[2] << 16 | (uint32_t)hi[3] << 24, hi[4] | hi[5] << 8 | hi[6] << 16 | (uint32_t)hi[7] << 24);
+                *reinterpret_cast<uint2 *>(smem + kOffCodeQ + code_off(8 + g, k0)) = make_uint2(lo[0] | lo[1] << 8 | lo[2] << 16 | (uint32_t)lo[3] << 24, lo[4] | lo[5] << 8 | lo[6] << 16 | (uint32_t)lo[7] << 24);
+                if ((r & 15) == 0) red[g] = __uint_as_float((uint32_t)(127 - up) << 23) * c2;
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");       // generic writes -> tensor-core reads
+            mbar_arrive(bar(kBarCodeQ));
+            softmax_sync();
+#pragma unroll
+            for (int q = 0; q < G; ++q) unscale[q] = red[q];
+            softmax_sync();                              // `red` is used again
+        }
+        // a query's score of this thread's row, in the base-2 domain
+        auto score = [&](const uint32_t (&acc)[16], int g) -> float {
+            if constexpr (kCodes) return fmaf(__uint_as_float(acc[8 + g]), 0.0625f, __uint_as_float(acc[g])) * unscale[g];
+            return __uint_as_float(acc[g]) * c2;
+        };
         float m[G], l[G], m0[G], l0[G];              // of the present chunk, and of the first
 #pragma unroll
         for (int g = 0; g < G; ++g) m0[g] = -INFINITY, l0[g] = 0.f;
@@ -476,7 +574,7 @@ attend_tc_kernel(Args p, const __grid_constant__ MapsFor<Args> maps)
                     const bool valid = seen(done + t, r);
 #pragma unroll
                     for (int g = 0; g < G; ++g)
-                        if (valid) m[g] = fmaxf(m[g], __uint_as_float(acc[g]) * c2);
+                        if (valid) m[g] = fmaxf(m[g], score(acc, g));
                 }
             }
 #pragma unroll
@@ -504,7 +602,16 @@ attend_tc_kernel(Args p, const __grid_constant__ MapsFor<Args> maps)
 #pragma unroll
                 for (int g = 0; g < G; ++g) {
                     // (a NaN or infinite score of a row that is not cached never gets here: `valid` decides)
-                    const float w = valid ? exp2f(__uint_as_float(acc[g]) * c2 - m[g]) : 0.f;
+                    const float w = valid ? exp2f(score(acc, g) - m[g]) : 0.f;
+                    if constexpr (kCodes) {
+                        uint8_t hi, lo;
+                        float value;
+                        two_codes(w * 256.f, &hi, &lo, &value);
+                        l[g] += value;                   // (of weights times 256, like the products)
+                        pt_smem[code_off(g, r)] = hi;
+                        pt_smem[code_off(8 + g, r)] = lo;
+                        continue;
+                    }
                     const __nv_bfloat16 hi = __float2bfloat16_rn(w);
                     const __nv_bfloat16 lo = __float2bfloat16_rn(w - __bfloat162float(hi));
                     l[g] += __bfloat162float(hi) + __bfloat162float(lo);
@@ -514,14 +621,14 @@ attend_tc_kernel(Args p, const __grid_constant__ MapsFor<Args> maps)
                 if (!kFp8 && !valid) {
                     // a row beyond the sequence's length may hold anything, and 0 x NaN would spoil the product: its V row
                     // is cleared in shared memory (only the split's last tile has such rows)
-                    const int s = i % kTcStages;
-                    ok = mbar_wait(bar(kBarFull + s), (i / kTcStages) & 1, abort_flag, sink);
+                    const int s = i % kStages;
+                    ok = mbar_wait(bar(kRingFull + s), (i / kStages) & 1, abort_flag, sink);
                     if (ok) {
-                        uint8_t *vt = smem + kOffRing + s * kTcTileBytes;
+                        uint8_t *vt = smem + kOffRing + s * kTileRoom;
 #pragma unroll
                         for (int x = 0; x < 8; ++x) {
                             *reinterpret_cast<uint4 *>(vt + r * 128 + x * 16) = make_uint4(0u, 0u, 0u, 0u);
-                            *reinterpret_cast<uint4 *>(vt + kTcHalf + r * 128 + x * 16) = make_uint4(0u, 0u, 0u, 0u);
+                            if (!kCodes) *reinterpret_cast<uint4 *>(vt + kTcHalf + r * 128 + x * 16) = make_uint4(0u, 0u, 0u, 0u);
                         }
                     }
                 }
@@ -563,9 +670,11 @@ attend_tc_kernel(Args p, const __grid_constant__ MapsFor<Args> maps)
         }
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-            const float den = ok ? (red[g] + red[8 + g]) + (red[16 + g] + red[24 + g]) : 0.f;     // error path: zeros
-            float num = __uint_as_float(o[g]) + __uint_as_float(o[8 + g]);
-            if (chunks > 1) num = (__uint_as_float(o0[g]) + __uint_as_float(o0[8 + g])) * w0[g] + num * w1[g];
+            float den = ok ? (red[g] + red[8 + g]) + (red[16 + g] + red[24 + g]) : 0.f;     // error path: zeros
+            constexpr float kLow = kCodes ? 0.0625f : 1.f;    // what the second part counts
+            float num = fmaf(__uint_as_float(o[8 + g]), kLow, __uint_as_float(o[g]));
+            if (chunks > 1) num = fmaf(__uint_as_float(o0[8 + g]), kLow, __uint_as_float(o0[g])) * w0[g] + num * w1[g];
+            if (kCodes) num *= 1.f / 256.f, den *= 1.f / 256.f;
             if (r >= kDim) continue;                          // (64 dimensions: the padded half of the output)
             if (!merges) {
                 put(out + (size_t)g * kDim + r, den > 0.f ? num / den : 0.f);
@@ -683,7 +792,8 @@ cudaError_t launch_tc_form(const Args &p, int heads, const MapsFor<Args> &maps, 
 template <int G, class Args>
 cudaError_t launch_tc_for(const Args &p, int heads, int src, const MapsFor<Args> &maps, cudaStream_t s)
 {
-    return src == 1 ? launch_tc_form<G, 1, Args>(p, heads, maps, s) : src == 2 ? launch_tc_form<G, 2, Args>(p, heads, maps, s)
+    constexpr int kFp8Src = std::is_same<Args, AttendTcMore>::value ? 3 : 1;
+    return src == 1 ? launch_tc_form<G, kFp8Src, Args>(p, heads, maps, s) : src == 2 ? launch_tc_form<G, 2, Args>(p, heads, maps, s)
                                                                            : launch_tc_form<G, 0, Args>(p, heads, maps, s);
 }
 
