@@ -150,7 +150,7 @@ int plan_window(const rkv_desc_t *d, int budget, int buffer, const rkv_tokens_t 
     x->single = !tokens->offsets && tokens->longest == 1 && back_to_back(d, tokens->q_stride) && back_to_back(d, tokens->out_stride) &&
                 attend_more_supported(d->dtype, d->head_dim, p->group, tiles);
     if (x->single) {
-        attend_more_plan(p, d->dtype, tiles, sm_count(), false, &x->separate);
+        attend_more_plan(p, tiles, sm_count(), false, &x->separate);
         p->slots = x->separate ? p->splits : 0;
         x->wide = x->bytes = x->separate ? part_bytes(*p) : 0;
     } else {
@@ -195,7 +195,7 @@ int plan_prefix(const rkv_desc_t *d, int budget, int buffer, const rkv_prefix_t 
     own->joined = (again <= kReadAgainBytes || d->batch == x->count) && attend_more_supported(d->dtype, d->head_dim, p->group, with_prefix);
     own->tiles = own->joined ? with_prefix : tiles;
     own->single = own->joined || attend_more_supported(d->dtype, d->head_dim, p->group, tiles);
-    if (own->single) attend_more_plan(p, d->dtype, own->tiles, sms, !own->joined, &own->separate);
+    if (own->single) attend_more_plan(p, own->tiles, sms, !own->joined, &own->separate);
     else p->splits = splits_for(d, *p, sms);
     if (own->joined) {
         p->slots = own->separate ? p->splits : 0;

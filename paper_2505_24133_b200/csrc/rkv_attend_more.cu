@@ -15,15 +15,14 @@ bool attend_more_supported(int dtype, int d, int group, long long tiles)
     return dtype != RKV_F32 && attend_supported(group, dtype, d) && tiles <= (long long)kTcMaxSplits * 2 * kTcChunkTiles;
 }
 
-// Splits as for rkv_decode_attention; blocks of their own where those are the faster there (attend_tc_separate), and beside another
-// kernel where not all blocks are on the GPU at a time: a block that waited for the other kernel's results would keep the next one out (256
-// sequences of 1152 rows and four prefixes of 16000: 259 us; 64 of 580 and 2048: 60 us).
-void attend_more_plan(RowsParams *p, int dtype, long long tiles, int sms, bool others, bool *separate)
+// Splits as for rkv_decode_attention.  They are a cluster, but beside another kernel, where not all blocks are on the GPU at a time, blocks of their
+// own: one that waited for the other kernel's results would keep the next block out (256 sequences of 1152 rows and four prefixes of 16000:
+// 259 us, 238 with a merge kernel; 64 of 580 and one of 2048: 60, 45).
+void attend_more_plan(RowsParams *p, long long tiles, int sms, bool others, bool *separate)
 {
     const int heads = p->tokens.count * p->hkv;
     p->splits = attend_tc_splits(heads, (int)tiles * kTile, sms);
     *separate = others && (long long)heads * p->splits > 2ll * sms;
-    *separate = *separate || p->splits > 1 && source_of(dtype, p->d) == 2 && (long long)heads * p->splits > 4ll * sms;
 }
 
 cudaError_t launch_attend_more(const RowsParams &r, int dtype, long long tiles, bool separate, int others, bool late, const RowsParams *prefix,

@@ -41,6 +41,9 @@
 // the largest to 2^-21 of it.  A weight times 256 is held to 2^-8 of itself, as one bf16 part would hold it (to 2^-22 in all where that
 // is more); the sum of the weights is taken from the parts.
 //
+// Of 64 dimensions, as they are stored (kHalf, the calls of AttendTcMore): the tiles go to the tensor cores as they land, too, keys as four steps of 16
+// columns, values as the lower half of M.
+//
 // Every mbarrier wait is bounded; on expiry the block records RKV_ERR_TIMEOUT,
 // writes zeros and leaves through the common exit that frees TMEM.  No TMA multicast.
 #pragma once
@@ -69,7 +72,7 @@ constexpr uint32_t kTcTmemCols = 256;                // 16 (output) per chunk + 
 constexpr int kOffRing = 0;                          // bf16 caches: kTcStages tiles.  8-bit caches: kConvBufs widened tiles,
 constexpr int kConvBufs = 2;
 constexpr int kRawStages = 2;
-constexpr int kCodeStages = 6;                       // ring of tiles of codes as they are stored, in the room of kTcStages bf16 ones
+constexpr int kCodeStages = 6;                       // ring of 16 KB tiles as they are stored, in the room of kTcStages of 32 KB
 constexpr int kOffRaw = kConvBufs * kTcTileBytes;    // then kRawStages raw stages of 16 KB
 constexpr int kRawBytes = kTile * kHeadDim;          // a tile of E4M3 codes
 constexpr int kOffQ = kOffRing + kTcStages * kTcTileBytes;
@@ -195,7 +198,7 @@ __device__ __forceinline__ void umma_codes(uint32_t d_tmem, uint64_t a_desc, uin
 //           (1024 heads of 9 tiles, three quarters of the sequences empty: 25.4 us, and 32.2 with the early tiles).
 //   kTwo    blocks of more tiles than one chunk takes
 // kSrc: 0 = bf16 caches of 128 dimensions (tiles go to the tensor cores as they land), 1 = E4M3 codes of 128 dimensions,
-// 3 = E4M3 codes of 128 dimensions as they are stored (AttendTcMore), 2 = bf16 caches of 64 dimensions (1 and 2: rows of 128 bytes, widened / padded with zeros into bf16 operand tiles of
+// 3 = E4M3 codes of 128 dimensions, 4 = bf16 caches of 64 dimensions, both as they are stored (AttendTcMore), 2 = bf16 caches of 64 dimensions (1 and 2: rows of 128 bytes, widened / padded with zeros into bf16 operand tiles of
 // 128 dimensions; the queries of the 64-dimension case fill the first half of their operand, the rest stays zero).
 enum { kPlain, kEarly, kTwo };
 template <int G, int kSrc, int kForm, class Args>
@@ -204,9 +207,11 @@ attend_tc_kernel(Args p, const __grid_constant__ MapsFor<Args> maps)
 {
     constexpr bool kFp8 = kSrc == 1 || kSrc == 2;            // the tiles pass through the softmax threads on their way to the tensor cores
     constexpr bool kCodes = kSrc == 3;          // E4M3 codes as they are stored
-    constexpr int kStages = kCodes ? kCodeStages : kTcStages, kTileRoom = kCodes ? kRawBytes : kTcTileBytes;
-    constexpr int kRingFull = kCodes ? (int)kBarCodeFull : (int)kBarFull, kRingEmpty = kCodes ? (int)kBarCodeEmpty : (int)kBarEmpty;
-    constexpr int kDim = kSrc == 2 ? 64 : kHeadDim;          // head dimension of the caches, the queries and the output
+    constexpr bool kHalf = kSrc == 4;           // bf16 rows of 64 dimensions as they are stored
+    constexpr bool kNarrow = kCodes || kHalf;   // tiles of 16 KB as they land
+    constexpr int kStages = kCodes ? kCodeStages : kHalf ? kCodeStages - 1 : kTcStages, kTileRoom = kNarrow ? kRawBytes : kTcTileBytes;
+    constexpr int kRingFull = kNarrow ? (int)kBarCodeFull : (int)kBarFull, kRingEmpty = kNarrow ? (int)kBarCodeEmpty : (int)kBarEmpty;
+    constexpr int kDim = kSrc == 2 || kSrc == 4 ? 64 : kHeadDim;          // head dimension of the caches, the queries and the output
     constexpr bool kMore = std::is_same<Args, AttendTcMore>::value;
     constexpr bool kSeparate = kFp8 || kMore;   // the splits may be blocks of their own
     using Out = typename std::conditional<kMore, __nv_bfloat16, float>::type;
@@ -232,8 +237,8 @@ attend_tc_kernel(Args p, const __grid_constant__ MapsFor<Args> maps)
             mbar_init(bar(kBarRawFull + s), 1);
             mbar_init(bar(kBarRawEmpty + s), 128);
         }
-        if (kCodes) {
-            for (int s = 0; s < kCodeStages; ++s) {
+        if (kNarrow) {
+            for (int s = 0; s < kStages; ++s) {
                 mbar_init(bar(kBarCodeFull + s), 1);
                 mbar_init(bar(kBarCodeEmpty + s), 1);
             }
@@ -301,8 +306,8 @@ attend_tc_kernel(Args p, const __grid_constant__ MapsFor<Args> maps)
             const int s = i % kRawStages;
             mbar_expect_tx(bar(kBarRawFull + s), kRawBytes);
             tma_load_2d(sbase + kOffRaw + s * kRawBytes, map, 0, y, bar(kBarRawFull + s));
-        } else if (kCodes) {
-            const int s = i % kCodeStages;
+        } else if (kNarrow) {
+            const int s = i % kStages;
             mbar_expect_tx(bar(kBarCodeFull + s), kRawBytes);
             tma_load_2d(sbase + kOffRing + s * kRawBytes, map, 0, y, bar(kBarCodeFull + s));
         } else {
@@ -314,10 +319,10 @@ attend_tc_kernel(Args p, const __grid_constant__ MapsFor<Args> maps)
         }
     };
     auto fetch_queries = [&]() {
-        mbar_expect_tx(bar(kBarQ), kSrc == 2 ? kTcSmall / 2 : kTcSmall);
+        mbar_expect_tx(bar(kBarQ), kDim == 64 ? kTcSmall / 2 : kTcSmall);
         const int qy = b * p.hq + h * G;                 // the group's G query rows (the rows after them are not used)
         tma_load_2d(sbase + kOffQ, &maps.q, 0, qy, bar(kBarQ));
-        if (kSrc != 2) tma_load_2d(sbase + kOffQ + kTcSmall / 2, &maps.q, 64, qy, bar(kBarQ));
+        if (kDim != 64) tma_load_2d(sbase + kOffQ + kTcSmall / 2, &maps.q, 64, qy, bar(kBarQ));
     };
     if (kForm == kEarly && warp == 4 && lane == 0) {
         fetch_queries();
@@ -437,7 +442,9 @@ attend_tc_kernel(Args p, const __grid_constant__ MapsFor<Args> maps)
                     ok = mbar_wait(bar(kRingFull + s), (i / kBufs) & 1, abort_flag, sink);
                     if (!ok) break;
                     tc_fence_after();
-                    if (kCodes)
+                    if (kHalf)
+                        umma_tile_k64(tmem + 16 * (chunks + t), sbase + kOffRing + s * kRawBytes, sbase + kOffQ, idesc_s);
+                    else if (kCodes)
                         umma_tile_row128<true>(tmem + 16 * (chunks + t), sbase + kOffRing + s * kRawBytes, sbase + kOffCodeQ, idesc_s);
                     else
                         umma_tile_k128_halves(tmem + 16 * (chunks + t), sbase + kOffRing + s * kTcTileBytes, kTcHalf, sbase + kOffQ,
@@ -463,7 +470,9 @@ attend_tc_kernel(Args p, const __grid_constant__ MapsFor<Args> maps)
                         umma_commit(bar(kBarPEmpty + pb));
                         continue;
                     }
-                    const uint32_t v_tile = sbase + kOffRing + s * kTcTileBytes, p_tile = sbase + kOffP + pb * kTcSmall;
+                    // (64 dimensions as they are stored: the upper half of M is the next stage of the ring, whatever it holds; its rows of the
+                    // output are nobody's)
+                    const uint32_t v_tile = sbase + kOffRing + s * kTileRoom, p_tile = sbase + kOffP + pb * kTcSmall;
 #pragma unroll
                     for (int ks = 0; ks < 8; ++ks) {         // 16 keys per step
                         const uint32_t a_addr = v_tile + ks * 2048;             // 16 rows of 128 bytes further
@@ -628,7 +637,7 @@ attend_tc_kernel(Args p, const __grid_constant__ MapsFor<Args> maps)
 #pragma unroll
                         for (int x = 0; x < 8; ++x) {
                             *reinterpret_cast<uint4 *>(vt + r * 128 + x * 16) = make_uint4(0u, 0u, 0u, 0u);
-                            if (!kCodes) *reinterpret_cast<uint4 *>(vt + kTcHalf + r * 128 + x * 16) = make_uint4(0u, 0u, 0u, 0u);
+                            if (!kNarrow) *reinterpret_cast<uint4 *>(vt + kTcHalf + r * 128 + x * 16) = make_uint4(0u, 0u, 0u, 0u);
                         }
                     }
                 }
@@ -792,8 +801,8 @@ cudaError_t launch_tc_form(const Args &p, int heads, const MapsFor<Args> &maps, 
 template <int G, class Args>
 cudaError_t launch_tc_for(const Args &p, int heads, int src, const MapsFor<Args> &maps, cudaStream_t s)
 {
-    constexpr int kFp8Src = std::is_same<Args, AttendTcMore>::value ? 3 : 1;
-    return src == 1 ? launch_tc_form<G, kFp8Src, Args>(p, heads, maps, s) : src == 2 ? launch_tc_form<G, 2, Args>(p, heads, maps, s)
+    constexpr bool kMore = std::is_same<Args, AttendTcMore>::value;
+    return src == 1 ? launch_tc_form<G, kMore ? 3 : 1, Args>(p, heads, maps, s) : src == 2 ? launch_tc_form<G, kMore ? 4 : 2, Args>(p, heads, maps, s)
                                                                            : launch_tc_form<G, 0, Args>(p, heads, maps, s);
 }
 
