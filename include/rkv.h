@@ -349,7 +349,7 @@ typedef struct rkv_rotary {
  * Products in fp32, rounded once; what is not rotated and keeps its type is copied bit for bit.  All tensors 16-byte aligned.
  * A sequence that the tokens do not fit into (or whose length is invalid), or whose positions leave the table, is left as it is, its rows of q_out
  * too, and RKV_ERR_INVALID_ARG is written to desc->device_status.
- * One launch for one token per sequence (offsets NULL, longest 1), else two; no workspace.
+ * One launch for one token or a few per sequence, else two; no workspace.
  */
 RKV_API int rkv_append_rotary(const rkv_desc_t *desc, void *k_cache, void *v_cache, const void *k_new, const void *v_new,
                               int32_t *seq_lens, int32_t budget, int32_t buffer, const rkv_tokens_t *tokens,

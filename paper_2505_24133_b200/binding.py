@@ -262,11 +262,13 @@ def _token_rows(t, stride: int):
     """The data pointer of a token tensor [total, heads, head_dim] whose rows are `stride` elements apart (0: contiguous)."""
     if t is None or isinstance(t, int) or stride == 0:
         return t                     # (a tensor's contiguity is checked where its pointer is taken)
-    row = 1
-    for size, step in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
-        assert size == 1 or step == row, "a token's heads must lie back to back"
-        row *= size
-    assert t.shape[0] <= 1 or t.stride(0) == stride, "the tensor's rows are not the tokens' stride apart"
+    steps = t.stride()
+    if steps[0] != stride or steps[-1] != 1 or len(steps) != 3 or steps[1] != t.shape[2]:      # (axes of one entry have any step)
+        row = 1
+        for size, step in zip(reversed(t.shape[1:]), reversed(steps[1:])):
+            assert size == 1 or step == row, "a token's heads must lie back to back"
+            row *= size
+        assert t.shape[0] <= 1 or steps[0] == stride, "the tensor's rows are not the tokens' stride apart"
     return t.data_ptr()
 
 
@@ -276,9 +278,10 @@ def rkv_append_rotary(desc, k_cache, v_cache, k_new, v_new, seq_lens, budget, bu
     queries, where given, are rotated into q_out; seq_lens[b] grows by the sequence's new tokens."""
     if _fast is None:
         lib()
-    return _fast.append_rotary(desc, k_cache, v_cache, _token_rows(k_new, tokens.k_stride), _token_rows(v_new, tokens.v_stride),
-                               seq_lens, budget, buffer, tokens, rotary, _token_rows(q_new, tokens.q_stride),
-                               _token_rows(q_out, tokens.out_stride), stream)
+    if tokens.k_stride or tokens.v_stride or tokens.q_stride or tokens.out_stride:
+        k_new, v_new = _token_rows(k_new, tokens.k_stride), _token_rows(v_new, tokens.v_stride)
+        q_new, q_out = _token_rows(q_new, tokens.q_stride), _token_rows(q_out, tokens.out_stride)
+    return _fast.append_rotary(desc, k_cache, v_cache, k_new, v_new, seq_lens, budget, buffer, tokens, rotary, q_new, q_out, stream)
 
 
 def rkv_window_workspace_bytes(desc, budget: int, buffer: int, tokens: RkvTokens, window: int, sinks: int) -> int:
@@ -290,8 +293,9 @@ def rkv_window_attention(desc, k_cache, v_cache, q, seq_lens, out, budget, buffe
     `window` (0: all) or among the first `sinks`; out has q's shape and type."""
     if _fast is None:
         lib()
-    return _fast.window_attention(desc, k_cache, v_cache, _token_rows(q, tokens.q_stride), seq_lens, _token_rows(out, tokens.out_stride),
-                                  budget, buffer, tokens, window, sinks, stream)
+    if tokens.q_stride or tokens.out_stride:
+        q, out = _token_rows(q, tokens.q_stride), _token_rows(out, tokens.out_stride)
+    return _fast.window_attention(desc, k_cache, v_cache, q, seq_lens, out, budget, buffer, tokens, window, sinks, stream)
 
 
 def rkv_prefix(k: torch.Tensor, v: torch.Tensor, lens: torch.Tensor, table: Optional[torch.Tensor] = None) -> RkvPrefix:
