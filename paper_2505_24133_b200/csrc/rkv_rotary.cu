@@ -11,7 +11,6 @@ namespace rkv {
 namespace {
 
 constexpr int kRotThreads = 256, kRotStepThreads = 512;
-constexpr int kAhead = 4;            // heads whose vectors a thread has under way
 
 // Eight consecutive elements of the token tensors as they lie, and as fp32.
 template <typename T> struct Vec8;
@@ -74,8 +73,11 @@ __device__ __forceinline__ int warp_find_sequence(const TokenMap &m, int t)
 // kStep: a block per sequence, for one token or a few; the length grows behind the block's own barrier.  Otherwise the warps of all blocks
 // take tokens one by one (warps_per_token to each) and bump_tokens_kernel below follows, 3 us and a launch more.
 template <typename T, bool kCodes, bool kStep>
-__global__ void __launch_bounds__(kStep ? kRotStepThreads : kRotThreads) append_rotary_kernel(RotaryParams p)
+__global__ void __launch_bounds__(kStep ? kRotStepThreads : kRotThreads, kStep ? 1 : kCodes || sizeof(T) == 4 ? 2 : 3) append_rotary_kernel(RotaryParams p)
 {
+    // Heads whose vectors a thread has under way.  16 prompts of 4096 tokens of 56 bf16 heads: 296 us with four and three blocks to an SM (0.98 of the
+    // copy rate), 317 with two blocks; into 8-bit pages 161 with four, 187 with two.  Single tokens 3.6 us with one, 4.0 with four.
+    constexpr int kAhead = kStep ? 1 : 4;
     constexpr int kWarps = (kStep ? kRotStepThreads : kRotThreads) / 32;
     pdl_trigger();
     pdl_wait();
