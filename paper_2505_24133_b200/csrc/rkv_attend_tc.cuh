@@ -279,7 +279,7 @@ attend_tc_kernel(Args p, const __grid_constant__ MapsFor<Args> maps)
 
     const int t0 = split * p.tiles_per_split;                       // first key tile of this block
     // where key tile t of the head starts, in rows of the 2-D [rows][d] view of the caches
-    KeyTiles keys;                          // (kMore: of the sequence's own rows, behind `prefix_tiles` of its prefix's `prefix_len` rows)
+    KeyTiles keys = {};                     // (kMore: of the sequence's own rows, behind `prefix_tiles` of its prefix's `prefix_len` rows)
     int prefix_tiles = 0, prefix_len = 0;
     auto tile_y = [&](int t) -> int {
         if constexpr (kMore) {
@@ -324,9 +324,12 @@ attend_tc_kernel(Args p, const __grid_constant__ MapsFor<Args> maps)
         tma_load_2d(sbase + kOffQ, &maps.q, 0, qy, bar(kBarQ));
         if (kDim != 64) tma_load_2d(sbase + kOffQ + kTcSmall / 2, &maps.q, 64, qy, bar(kBarQ));
     };
+    // kMore: with a window or a prefix the first tile depends on the lengths, and so does whether a page has to exist
+    bool early_tile = true;
+    if constexpr (kMore) early_tile = p.window == 0 && !p.prefix_lens && !p.block_table;
     if (kForm == kEarly && warp == 4 && lane == 0) {
         fetch_queries();
-        if (!kMore) fetch_tile(&maps.k, 0, tile_y(t0));       // (which tile is the first depends on the length there)
+        if (early_tile) fetch_tile(&maps.k, 0, tile_y(t0));
     }
     int L = p.seq_lens[b];
     bool short_of = false;
@@ -392,7 +395,7 @@ attend_tc_kernel(Args p, const __grid_constant__ MapsFor<Args> maps)
         if (kForm == kEarly) {                           // what is under way lands before the block's memory is given up
             if (warp == 4 && lane == 0) {
                 mbar_wait(bar(kBarQ), 0, abort_flag, sink);
-                if (!kMore) mbar_wait(bar(kFp8 ? kBarRawFull : kBarFull), 0, abort_flag, sink);
+                if (early_tile) mbar_wait(bar(kFp8 ? (int)kBarRawFull : kRingFull), 0, abort_flag, sink);
             }
             __syncwarp();
         }
@@ -413,7 +416,7 @@ attend_tc_kernel(Args p, const __grid_constant__ MapsFor<Args> maps)
         if (lane == 0) {
             constexpr int kRing = kFp8 ? kRawStages : kStages, kEmpty = kFp8 ? (int)kBarRawEmpty : kRingEmpty;
             if (kForm != kEarly) fetch_queries();
-            for (int i = kForm == kEarly && !kMore ? 1 : 0; i < 2 * T; ++i) {
+            for (int i = kForm == kEarly && early_tile ? 1 : 0; i < 2 * T; ++i) {
                 bool value;
                 const int t = t0 + source(i, &value), y = tile_y(t);
                 if (!mbar_wait(bar(kEmpty + i % kRing), ((i / kRing) & 1) ^ 1, abort_flag, sink)) break;

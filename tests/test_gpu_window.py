@@ -115,6 +115,15 @@ def test_one_token_per_sequence(rkv, dtype, d, window, sinks):
 
 
 @pytest.mark.parametrize("dtype,d", SHAPES)
+@pytest.mark.parametrize("window,sinks", [(0, 0), (100, 4), (300, 130)])
+@pytest.mark.parametrize("batch", [4, 90])
+def test_one_token_per_sequence_paged(rkv, dtype, d, window, sinks, batch):
+    """Pages behind the lengths and outside the windows do not exist, and nothing asks for them."""
+    lens = [1, 300, 640, 128] + [(53 * b) % 640 + 1 for b in range(batch - 4)]
+    Setup(rkv, dtype, d, 2, 8, lens, [1] * batch, 640, window, sinks, paged=True, offsets=False).run()
+
+
+@pytest.mark.parametrize("dtype,d", SHAPES)
 @pytest.mark.parametrize("window,sinks,paged", [(0, 0, False), (0, 9, True), (1, 1, True), (60, 4, False), (200, 130, True), (257, 0, True)])
 def test_ragged_prompts(rkv, dtype, d, window, sinks, paged):
     """Prompts and pieces of prompts of 0 to 300 tokens over caches that hold more, or nothing else."""
