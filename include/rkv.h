@@ -361,7 +361,7 @@ RKV_API int rkv_append_rotary(const rkv_desc_t *desc, void *k_cache, void *v_cac
  *   j <= r  with  r - j < window  or  j < sinks        (window 0: all j <= r)
  *   out[t][q] = sum_j softmax_j( q[t][q] . K[b][q / G][j] / sqrt(head_dim) ) V[b][q / G][j]
  *   q    [total][n_q_heads][head_dim] (device; desc->dtype, bf16 for 8-bit caches)
- *   out  the same shape and type as q (device); out_stride of `tokens` is its rows' distance
+ *   out  the same shape and type as q (device), not overlapping it; out_stride of `tokens` is its rows' distance
  *   window >= 0, sinks >= 0
  * Rows of the caches that no new token sees are not read, nor their pages' entries where a whole page of 128 rows is such, and may hold
  * anything; the rows that some new token sees hold finite values (a NaN or infinity there may reach every new token of the sequence).  A sequence

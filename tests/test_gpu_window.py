@@ -132,6 +132,21 @@ def test_ragged_prompts(rkv, dtype, d, window, sinks, paged):
     Setup(rkv, dtype, d, 2, 8, lens, new, 640, window, sinks, paged=paged, strided=True, behind=3).run()
 
 
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("fp8", 128), ("f32", 128)])
+def test_one_token_per_sequence_strided_or_with_gaps(rkv, dtype, d):
+    """Queries out of a wider projection; and a batch in which some sequences have no token in the call."""
+    Setup(rkv, dtype, d, 2, 6, [5, 200, 300], [1, 1, 1], 384, 100, 4, strided=True, offsets=False).run()
+    Setup(rkv, dtype, d, 2, 6, [5, 200, 300, 7], [1, 0, 1, 0], 384, 100, 4, behind=2).run()
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("fp8", 128)])
+def test_many_sequences_of_different_lengths(rkv, dtype, d):
+    """More items than blocks, most of them with few keys or none."""
+    new = [(37 * b) % 210 for b in range(150)]
+    lens = [n + (91 * b) % 300 for b, n in enumerate(new)]
+    Setup(rkv, dtype, d, 2, 8, lens, new, 512, 150, 4).run()
+
+
 @pytest.mark.parametrize("hkv,hq", [(1, 1), (3, 3), (2, 6), (1, 5), (2, 12), (1, 7), (2, 16), (1, 16), (1, 48), (1, 100), (1, 130)])
 @pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("fp8", 128), ("f32", 128)])
 def test_head_layouts(rkv, dtype, d, hkv, hq):
