@@ -70,14 +70,17 @@ __device__ __forceinline__ int warp_find_sequence(const TokenMap &m, int t)
     return lo < m.count ? lo : -1;
 }
 
-// kStep: a block per sequence, for one token or a few; the length grows behind the block's own barrier.  Otherwise the warps of all blocks
+// kOne, kFew: a block per sequence, for one token or a few; the length grows behind the block's own barrier.  Otherwise the warps of all blocks
 // take tokens one by one (warps_per_token to each) and bump_tokens_kernel below follows, 3 us and a launch more.
-template <typename T, bool kCodes, bool kStep>
-__global__ void __launch_bounds__(kStep ? kRotStepThreads : kRotThreads, kStep ? 1 : kCodes || sizeof(T) == 4 ? 2 : 3) append_rotary_kernel(RotaryParams p)
+enum { kMany, kOne, kFew };
+template <typename T, bool kCodes, int kMode>
+__global__ void __launch_bounds__(kMode != kMany ? kRotStepThreads : kRotThreads, kMode != kMany ? 1 : kCodes || sizeof(T) == 4 ? 2 : 3)
+append_rotary_kernel(RotaryParams p)
 {
     // Heads whose vectors a thread has under way.  16 prompts of 4096 tokens of 56 bf16 heads: 296 us with four and three blocks to an SM (0.98 of the
     // copy rate), 317 with two blocks; into 8-bit pages 161 with four, 187 with two.  Single tokens 3.6 us with one, 4.0 with four.
-    constexpr int kAhead = kStep ? 1 : 4;
+    constexpr int kAhead = kMode == kOne ? 1 : 4;
+    constexpr bool kStep = kMode != kMany;
     constexpr int kWarps = (kStep ? kRotStepThreads : kRotThreads) / 32;
     pdl_trigger();
     pdl_wait();
@@ -245,7 +248,7 @@ cudaError_t launch_type(RotaryParams p, cudaStream_t s)
     if (p.tokens.longest == 1 || (long long)p.tokens.longest * most <= 8 * kStepWarps) {
         p.warps_per_token = 1;
         while (p.warps_per_token < kStepWarps && p.warps_per_token < most && p.warps_per_token * p.tokens.longest < kStepWarps) p.warps_per_token *= 2;
-        return launch_early(append_rotary_kernel<T, kCodes, true>, (unsigned)p.tokens.count, kRotStepThreads, 0, s, 1, p);
+        return launch_early(p.tokens.longest == 1 ? append_rotary_kernel<T, kCodes, kOne> : append_rotary_kernel<T, kCodes, kFew>, (unsigned)p.tokens.count, kRotStepThreads, 0, s, 1, p);
     }
     // as many warps to a token as its heads keep busy, where the tokens alone do not fill the GPU (16 warps to each of 148 SMs)
     int wpt = 1;
@@ -253,7 +256,7 @@ cudaError_t launch_type(RotaryParams p, cudaStream_t s)
     p.warps_per_token = wpt;
     constexpr int kWarps = kRotThreads / 32;
     const long long blocks = ((long long)p.tokens.total * wpt + kWarps - 1) / kWarps;
-    const cudaError_t e = launch_early(append_rotary_kernel<T, kCodes, false>, (unsigned)blocks, kRotThreads, 0, s, 1, p);
+    const cudaError_t e = launch_early(append_rotary_kernel<T, kCodes, kMany>, (unsigned)blocks, kRotThreads, 0, s, 1, p);
     if (e != cudaSuccess) return e;
     return launch_early(bump_tokens_kernel, (unsigned)((p.tokens.count + kRotThreads - 1) / kRotThreads), kRotThreads, 0, s, 1, p);
 }
