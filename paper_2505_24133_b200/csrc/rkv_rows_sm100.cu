@@ -273,9 +273,9 @@ rows_tc_kernel(RowsParams p, int tokens_per_tile, int pieces, int items, const _
     // kernel waited for tensor memory, would wait for good.  (And only behind the wait above: see AttendTcMore::late.)
     pdl_trigger();
 
-    // The item behind the nth of this block, -1: none.
-    auto next_item = [&](int nth) -> int {
-        const bool there = __all_sync(0xffffffffu, mbar_wait(bar(S::kNext + (nth & 1)), (nth >> 1) & 1, abort_flag, sink));
+    // The item behind the nth of this block, -1: none, or a wait of one of the warp's lanes ran out.
+    auto next_item = [&](int nth, bool ok) -> int {
+        const bool there = __all_sync(0xffffffffu, ok && mbar_wait(bar(S::kNext + (nth & 1)), (nth >> 1) & 1, abort_flag, sink));
         const int idx = there ? read_next(sbase + S::kOffNext + 16 * (nth & 1)) : -1;
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
@@ -286,16 +286,16 @@ rows_tc_kernel(RowsParams p, int tokens_per_tile, int pieces, int items, const _
         // ------------------------------------------------------------------ TMA producer
         int base = 0, turn = 0, borders = 0;                             // tiles through the ring, items with keys, border tiles so far
         bool ok = true;
-        for (int nth = 0, idx = blockIdx.x; idx >= 0 && ok; idx = next_item(nth++)) {
+        for (int nth = 0, idx = blockIdx.x; idx >= 0; idx = next_item(nth++, ok)) {
             // the question for the next item, when the answer before the last has been read
             ok = __all_sync(0xffffffffu, mbar_wait(bar(S::kNextFree + (nth & 1)), ((nth >> 1) & 1) ^ 1, abort_flag, sink));
-            if (!ok) break;
+            if (!ok) continue;
             if (lane == 0) ask_next(sbase + S::kOffNext + 16 * (nth & 1), bar(S::kNext + (nth & 1)));
             Item x;
             if (!load_item(p, idx, items, kTiles * tokens_per_tile, pieces, lane == 0, &x) || x.T == 0) continue;
             const int head = x.b * p.hkv + x.h;
             const CallTiles call = call_tiles(p.causal, p.window, p.sinks, x.len, x.n);
-            ok = mbar_wait(bar(S::kQFree), (turn & 1) ^ 1, abort_flag, sink);
+            ok = __all_sync(0xffffffffu, mbar_wait(bar(S::kQFree), (turn & 1) ^ 1, abort_flag, sink));
             if (lane == 0 && ok) {
                 mbar_expect_tx(bar(S::kQ), kTiles * S::kHalves * 128 * tokens_per_tile * p.group);
                 for (int i = 0; i < kTiles; ++i)
@@ -380,7 +380,7 @@ rows_tc_kernel(RowsParams p, int tokens_per_tile, int pieces, int items, const _
                 if (r == kTiles - 1) umma_commit(bar(S::kEmpty + i % S::kStages));
             }
         };
-        for (int nth = 0, idx = blockIdx.x; idx >= 0 && ok; idx = next_item(nth++)) {
+        for (int nth = 0, idx = blockIdx.x; idx >= 0; idx = next_item(nth++, ok)) {
             Item x;
             if (!load_item(p, idx, items, kTiles * tokens_per_tile, pieces, false, &x) || x.T == 0) continue;
             T = x.T;
@@ -442,7 +442,7 @@ rows_tc_kernel(RowsParams p, int tokens_per_tile, int pieces, int items, const _
         bool ok = true;
         // (both warps of a pair go on, or neither: they wait for each other in every item)
         auto pair_next = [&](int nth) -> int {
-            int idx = next_item(nth), both;
+            int idx = next_item(nth, true), both;
             asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ge.s32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, %2, 64, p;\n\tselp.b32 %0, 1, 0, q;\n\t}"
                          : "=r"(both) : "r"(idx), "r"(1 + r * 4 + (warp & 3)) : "memory");
             return both ? idx : -1;

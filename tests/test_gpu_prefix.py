@@ -181,3 +181,61 @@ def test_another_stream_and_a_captured_graph(rkv):
     graph.replay()
     torch.cuda.synchronize()
     s.check()
+
+
+def _chain(rkv, wait):
+    """Steps of a batch of samples: append, attend over prefix and own rows, attend over a window; with `wait`, each call finished before the next."""
+    gen = torch.Generator(device="cuda").manual_seed(51)
+    B, hkv, hq, d, cap, rows = 48, 4, 16, 128, 256, 3000
+    draw = lambda *shape: torch.randn(*shape, generator=gen, device="cuda").to(torch.bfloat16)  # noqa: E731
+    k, v, pk, pv = draw(B, hkv, cap, d), draw(B, hkv, cap, d), draw(2, hkv, rows, d), draw(2, hkv, rows, d)
+    seq = torch.tensor([(5 * b) % 200 for b in range(B)], dtype=torch.int32, device="cuda")
+    plens = torch.tensor([rows, 2777], dtype=torch.int32, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    desc = descriptor(rkv, B, hkv, hq, d, "bf16", status)
+    prefix, tokens, rotary = rkv.rkv_prefix(pk, pv, plens), rkv.rkv_tokens(B, 1), rkv.rkv_rotary(None, 0)
+    room = torch.full((max(rkv.rkv_prefix_workspace_bytes(desc, cap - 1, 1, prefix), 256),), 0xFF, dtype=torch.uint8, device="cuda")
+    assert room.numel() > 256                                # (two kernels and partial results, not one)
+    desc.workspace, desc.workspace_bytes = room.data_ptr(), room.numel()
+    new = [(draw(B, hkv, d), draw(B, hkv, d), draw(B, hq, d)) for _ in range(12)]
+    outs = [(torch.empty(B, hq, d, dtype=torch.bfloat16, device="cuda"), torch.empty(B, hq, d, dtype=torch.bfloat16, device="cuda")) for _ in new]
+    torch.cuda.synchronize()
+    for (kn, vn, q), (a, w) in zip(new, outs):
+        calls = (lambda: rkv.rkv_append_rotary(desc, k, v, kn, vn, seq, cap - 1, 1, tokens, rotary),
+                 lambda: rkv.rkv_prefix_attention(desc, k, v, q, seq, a, cap - 1, 1, prefix),
+                 lambda: rkv.rkv_window_attention(desc, k, v, q, seq, w, cap - 1, 1, tokens, 50, 4))
+        for call in calls:
+            assert call() == 0
+            if wait:
+                torch.cuda.synchronize()
+    torch.cuda.synchronize()
+    assert int(status.item()) == 0
+    return [x for pair in outs for x in pair] + [k, v, seq]
+
+
+def test_steps_one_behind_the_other_equal_steps_with_waiting(rkv):
+    """The kernels of a step start early, beside the ones before them; what they compute is what they compute when each waits for the last."""
+    want = _chain(rkv, True)
+    for _ in range(3):
+        for a, b in zip(_chain(rkv, False), want):
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("fp8", 128), ("bf16", 64)])
+def test_two_calls_at_once(rkv, dtype, d):
+    """Calls with workspaces of their own on two streams give what they give one after the other."""
+    a = Setup(rkv, dtype, d, 2, 8, [(17 * b) % 250 for b in range(32)], [2000, 1500], 256, 2048, seed=42)
+    b = Setup(rkv, dtype, d, 2, 8, [(23 * b) % 250 for b in range(64)], [1800], 256, 2048, seed=43)
+    for s in (a, b):
+        assert s.call() == 0
+    torch.cuda.synchronize()
+    want = a.out.clone(), b.out.clone()
+    streams = torch.cuda.Stream(), torch.cuda.Stream()
+    a.out.zero_(), b.out.zero_()
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for s, st in zip((a, b), streams):
+            assert s.call(st) == 0
+    torch.cuda.synchronize()
+    assert torch.equal(a.out, want[0]) and torch.equal(b.out, want[1])
+    a.check(), b.check()

@@ -324,3 +324,29 @@ def test_append_then_attend_like_a_decode_loop(rkv):
     assert seq.tolist() == [budget, budget] and position.tolist() == [192, 153]
     step(rkv.rkv_tokens(B, 1), [1, 1])                       # positions go on where they were, rows where the compression left them
     assert seq.tolist() == [budget + 1, budget + 1] and position.tolist() == [193, 154]
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("fp8", 128), ("f32", 128)])
+def test_two_prompts_at_once(rkv, dtype, d):
+    """Calls with workspaces of their own on two streams, each of more items than the GPU takes at a time, give what they give one after the other."""
+    a = Setup(rkv, dtype, d, 2, 8, [900, 500, 70], [900, 500, 70], 1024, 0, 0, seed=44)
+    b = Setup(rkv, dtype, d, 2, 8, [1000, 30, 640], [1000, 30, 600], 1024, 200, 4, seed=45)
+    for s in (a, b):
+        assert s.call() == 0
+    torch.cuda.synchronize()
+    want = a.out.clone(), b.out.clone()
+    streams = torch.cuda.Stream(), torch.cuda.Stream()
+    a.out.zero_(), b.out.zero_()
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for s, st in zip((a, b), streams):
+            assert s.call(st) == 0
+    torch.cuda.synchronize()
+    assert torch.equal(a.out, want[0]) and torch.equal(b.out, want[1])
+    a.check(), b.check()
+
+
+def test_a_generous_bound_on_the_tokens(rkv):
+    """`longest` far above what any sequence has costs time, not results."""
+    Setup(rkv, "bf16", 128, 2, 8, [40, 259, 7], [40, 77, 0], 300, 50, 4, longest=20000).run()
+    Setup(rkv, "f32", 64, 2, 8, [40, 259, 7], [40, 77, 0], 300, 50, 4, longest=5000).run()
