@@ -150,7 +150,7 @@ int plan_window(const rkv_desc_t *d, int budget, int buffer, const rkv_tokens_t 
     x->single = !tokens->offsets && tokens->longest == 1 && back_to_back(d, tokens->q_stride) && back_to_back(d, tokens->out_stride) &&
                 attend_more_supported(d->dtype, d->head_dim, p->group, tiles);
     if (x->single) {
-        attend_more_plan(p, tiles, sm_count(), false, &x->separate);
+        attend_more_plan(p, d->dtype, tiles, sm_count(), false, &x->separate);
         p->slots = x->separate ? p->splits : 0;
         x->wide = x->bytes = x->separate ? part_bytes(*p) : 0;
     } else {
@@ -171,8 +171,10 @@ int check_prefix(const rkv_desc_t *d, const rkv_prefix_t *x)
 }
 
 // (Eager figures, one kernel and two: 8 sequences x 4 heads, 333 rows, 5 MB 9.1 us, 15.8; 32 x 8, 330 rows, 41 MB 13.5, 18.8; 4 x 8, 3000 rows, 47 MB
-// 17.4, 14.5; 64 x 8, 500 rows, 125 MB 27.7, 22.4; one sequence, 16000 rows 14.4, 25.3.)
-constexpr long long kReadAgainBytes = 48ll << 20;
+// 17.4, 14.5; 64 x 8, 500 rows, 125 MB 27.7, 22.4; one sequence, 16000 rows 14.4, 25.3.  Fp32 caches, whose prefixes go to the CUDA cores otherwise:
+// 32 x 8, 330 rows, 82 MB 45.8, 97.5; 4 x 8, 3000 rows, 94 MB 25.2, 35.6; 16 x 8, 2000 rows, 250 MB 57.5, 39.4; 64 x 8, 500 rows, 250 MB 88.8, 75.6;
+// 64 x 8, 1000 rows, 500 MB 113.9, 73.0.)
+constexpr long long kReadAgainBytes = 48ll << 20, kReadAgainBytesF32 = 160ll << 20;
 
 // shared: the prefixes' rows, whose partial results are a row's first slots; own: the sequences'.
 int plan_prefix(const rkv_desc_t *d, int budget, int buffer, const rkv_prefix_t *x, RowsParams *shared, Plan *own)
@@ -192,12 +194,14 @@ int plan_prefix(const rkv_desc_t *d, int budget, int buffer, const rkv_prefix_t 
     p->tokens = TokenMap{nullptr, d->batch, d->batch, 1};
     // Prefixes of few rows or few sequences are read again for every sequence, mostly from L2: one kernel instead of two, the second of which
     // waits for the first.
-    const long long again = (long long)d->batch * d->n_kv_heads * x->rows * 2 * d->head_dim * (d->dtype == RKV_BF16 ? 2 : 1);
+    const long long elem = d->dtype == RKV_F32 ? 4 : d->dtype == RKV_BF16 ? 2 : 1;
+    const long long again = (long long)d->batch * d->n_kv_heads * x->rows * 2 * d->head_dim * elem;
     const long long tiles = tiles_seen(*p, 1), with_prefix = tiles + tiles_seen(*shared, 1);
-    own->joined = (again <= kReadAgainBytes || d->batch == x->count) && attend_more_supported(d->dtype, d->head_dim, p->group, with_prefix);
+    own->joined = (again <= (d->dtype == RKV_F32 ? kReadAgainBytesF32 : kReadAgainBytes) || d->batch == x->count) &&
+                  attend_more_supported(d->dtype, d->head_dim, p->group, with_prefix);
     own->tiles = own->joined ? with_prefix : tiles;
     own->single = own->joined || attend_more_supported(d->dtype, d->head_dim, p->group, tiles);
-    if (own->single) attend_more_plan(p, own->tiles, sms, !own->joined, &own->separate);
+    if (own->single) attend_more_plan(p, d->dtype, own->tiles, sms, !own->joined, &own->separate);
     else p->splits = splits_for(d, *p, sms);
     if (own->joined) {
         p->slots = own->separate ? p->splits : 0;

@@ -17,7 +17,13 @@
 // An eighth warp is the producer of the bulk copies; stages are handed back through mbarriers.
 // With few head-problems the rows of a head are cut into splits (more blocks than SMs); a second small kernel merges
 // the splits' partial results.
+//
+// rkv_window_attention's single tokens and rkv_prefix_attention over fp32 caches (kMore): the rows that the token sees -- its prefix's, the
+// first ones, the window's -- one after the other, in tiles of 56 that are copied in as many runs as they have.  Nothing has to be masked.
+#include <type_traits>
+
 #include "rkv_sm100.cuh"
+#include "rkv_tokens.cuh"
 
 namespace rkv {
 
@@ -42,10 +48,20 @@ struct AttendParams {
     const int32_t *block_table;  // paged caches: [P][cap / 128] page ids (a page = 128 rows), else null
     int d_out;                   // head dimension of the output rows (the partial results always have rows of 128 + 2)
 };
+struct AttendMore : AttendParams {
+    int least, window, sinks;    // a length below `least` is an error; own rows seen: [0, sinks) and the last `window` (0: all)
+    long long pool_pages;
+    const void *prefix_k, *prefix_v;             // as rkv_prefix_t; sequence b has prefix b / per_prefix; prefix_lens null: none
+    const int32_t *prefix_lens, *prefix_table;
+    long long prefix_pages;
+    int prefix_cap, per_prefix;
+    int slot, slots;             // a row's partial results are slots slot .. of `slots` in `partial` (see RowsParams); partial null: `out` is written
+};
 
-template <typename T, int G>
-__global__ void __launch_bounds__(kAttThreads, (G <= 4 && sizeof(T) == 2) ? 2 : 1) attend_kernel(AttendParams p)
+template <typename T, int G, class Args>
+__global__ void __launch_bounds__(kAttThreads, (G <= 4 && sizeof(T) == 2) ? 2 : 1) attend_kernel(Args p)
 {
+    constexpr bool kMore = std::is_same<Args, AttendMore>::value;
     constexpr int kRowBytes = kHeadDim * (int)sizeof(T);
     constexpr int kTileBytesT = kAttRows * kRowBytes;
     constexpr int kPerVec = Elem<T>::kPerVec;               // elements per 16-byte vector
@@ -64,9 +80,22 @@ __global__ void __launch_bounds__(kAttThreads, (G <= 4 && sizeof(T) == 2) ? 2 : 
     const int b = head / p.hkv, h = head % p.hkv;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int L = p.seq_lens[b];
-    const bool bad_len = L < 0 || L > p.cap;
+    bool bad_len = L < 0 || L > p.cap;
+    if constexpr (kMore) bad_len = bad_len || L < p.least;
     if (bad_len && threadIdx.x == 0 && split == 0 && h == 0) report(p.status, RKV_ERR_INVALID_ARG);
-    const int Lc = bad_len ? 0 : L;
+    int Lc = bad_len ? 0 : L;            // rows that the query sees
+    int prefix_len = 0, first_len = 0, from = 0;         // kMore: the prefix's, the first of its own, then its own from row `from` on
+    if constexpr (kMore) {
+        if (p.window > 0) from = max(0, Lc - p.window), first_len = min(p.sinks, from);
+        if (p.prefix_lens) {
+            prefix_len = p.prefix_lens[b / p.per_prefix];
+            if (prefix_len < 0 || prefix_len > p.prefix_cap) {
+                if (threadIdx.x == 0 && split == 0) report(p.status, RKV_ERR_INVALID_ARG);
+                prefix_len = 0;
+            }
+        }
+        Lc = prefix_len + first_len + Lc - from;
+    }
     // this block's rows: whole tiles, split evenly
     const int tiles_all = (Lc + kAttRows - 1) / kAttRows;
     const int t_begin = (int)((long long)split * tiles_all / p.splits), t_end = (int)((long long)(split + 1) * tiles_all / p.splits);
@@ -104,6 +133,63 @@ __global__ void __launch_bounds__(kAttThreads, (G <= 4 && sizeof(T) == 2) ? 2 : 
                 const int row0 = (t_begin + t) * kAttRows;
                 const int rows = min(kAttRows, Lc - row0);
                 const uint32_t bar = smem_u32(bars + s);
+                if constexpr (kMore) {
+                    // the run that starts at the tile's row r: where it lies, and its length; rows of a page that does not exist are zeros
+                    auto run_at = [&](int r, const T **k, const T **v) -> int {
+                        int x = row0 + r, len, page_rows = kTile;
+                        const bool shared = x < prefix_len;
+                        if (shared) {
+                            len = prefix_len - x;
+                        } else if ((x -= prefix_len) < first_len) {
+                            len = first_len - x;
+                        } else {
+                            len = rows;                      // (to the tile's end at most)
+                            x += from - first_len;
+                        }
+                        const int cache = shared ? b / p.per_prefix * p.hkv + h : head, cap = shared ? p.prefix_cap : p.cap;
+                        const int32_t *table = shared ? p.prefix_table : p.block_table;
+                        long long at = (long long)cache * cap + x;
+                        if (table) {
+                            const int page = table[(size_t)cache * (cap / kTile) + x / kTile];
+                            page_rows = kTile - x % kTile;
+                            len = min(len, page_rows);
+                            at = page >= 0 && page < (shared ? p.prefix_pages : p.pool_pages) ? (long long)page * kTile + x % kTile : -1;
+                        }
+                        *k = at < 0 ? nullptr : static_cast<const T *>(shared ? p.prefix_k : p.k_cache) + at * kHeadDim;
+                        *v = at < 0 ? nullptr : static_cast<const T *>(shared ? p.prefix_v : p.v_cache) + at * kHeadDim;
+                        return min(len, rows - r);
+                    };
+                    uint8_t *tile = att_smem + (size_t)s * 2 * kTileBytesT;
+                    const T *k, *v;
+                    uint32_t there = 0;
+                    for (int r = 0; r < rows;) {
+                        const int n = run_at(r, &k, &v);
+                        if (k) {
+                            there += (uint32_t)n;
+                        } else {
+                            report(p.status, RKV_ERR_INVALID_ARG);
+                            for (int x = 0; x < n * kRowBytes / 16; ++x) {
+                                reinterpret_cast<uint4 *>(tile + (size_t)r * kRowBytes)[x] = make_uint4(0u, 0u, 0u, 0u);
+                                reinterpret_cast<uint4 *>(tile + kTileBytesT + (size_t)r * kRowBytes)[x] = make_uint4(0u, 0u, 0u, 0u);
+                            }
+                        }
+                        r += n;
+                    }
+                    if (there < (uint32_t)rows) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // before a later tile's copies
+                    mbar_expect_tx(bar, 2u * there * kRowBytes);
+                    for (int r = 0; r < rows;) {
+                        const int n = run_at(r, &k, &v);
+                        if (k) {
+                            const uint32_t bytes = (uint32_t)n * kRowBytes, off = (uint32_t)r * kRowBytes;
+                            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                                         ::"r"(smem_u32(tile) + off), "l"(k), "r"(bytes), "r"(bar) : "memory");
+                            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                                         ::"r"(smem_u32(tile + kTileBytesT) + off), "l"(v), "r"(bytes), "r"(bar) : "memory");
+                        }
+                        r += n;
+                    }
+                    continue;
+                }
                 mbar_expect_tx(bar, 2u * (uint32_t)rows * kRowBytes);
                 // one copy per operand, or two where the tile crosses a page boundary of a paged cache
                 const int first = p.block_table ? min(rows, kTile - row0 % kTile) : rows;
@@ -279,7 +365,16 @@ __global__ void __launch_bounds__(kAttThreads, (G <= 4 && sizeof(T) == 2) ? 2 : 
             num = fmaf(f, fold[((size_t)w * G + g) * kHeadDim + c], num);
             den = fmaf(f, wstat[(w * G + g) * 2 + 1], den);
         }
-        if (p.splits == 1) {
+        if constexpr (kMore) {
+            const size_t row = (size_t)b * p.hq + (size_t)h * G + g;
+            if (!p.partial) {
+                p.out[row * kHeadDim + c] = den > 0.f ? num / den : 0.f;
+                continue;
+            }
+            float *part = p.partial + (row * p.slots + p.slot + split) * slot_floats(kHeadDim);
+            part[c] = num;
+            if (c == 0) part[kHeadDim] = m, part[kHeadDim + 1] = den;
+        } else if (p.splits == 1) {
             p.out[((size_t)b * p.hq + (size_t)h * G + g) * kHeadDim + c] = den > 0.f ? num / den : 0.f;
         } else {
             float *part = p.partial + (((size_t)head * p.splits + split) * G + g) * (kHeadDim + 2);
@@ -312,30 +407,30 @@ __global__ void __launch_bounds__(kHeadDim) attend_merge_kernel(AttendParams p, 
     if (c < p.d_out) p.out[((size_t)b * p.hq + (size_t)h * G + g) * p.d_out + c] = den > 0.f ? num / den : 0.f;
 }
 
-template <typename T, int G>
-cudaError_t launch_one(const AttendParams &p, cudaStream_t s)
+template <typename T, int G, class Args>
+cudaError_t launch_one(const Args &p, cudaStream_t s)
 {
     const int tile_bytes = kAttRows * kHeadDim * (int)sizeof(T);
     const int smem = kAttStages * 2 * tile_bytes + (kAttWarps * (kAttRows / kAttWarps) * ((G + 3) / 4 * 4) + kAttWarps * G * 2) * 4 +
                      2 * kAttStages * 8 + 16;
-    cudaError_t e = cudaFuncSetAttribute(attend_kernel<T, G>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    cudaError_t e = cudaFuncSetAttribute(attend_kernel<T, G, Args>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
-    attend_kernel<T, G><<<(unsigned)(p.batch * p.hkv * p.splits), kAttThreads, smem, s>>>(p);
+    attend_kernel<T, G, Args><<<(unsigned)(p.batch * p.hkv * p.splits), kAttThreads, smem, s>>>(p);
     return cudaGetLastError();
 }
 
-template <typename T>
-cudaError_t launch_dtype(const AttendParams &p, int G, cudaStream_t s)
+template <typename T, class Args>
+cudaError_t launch_dtype(const Args &p, int G, cudaStream_t s)
 {
     switch (G) {
-        case 1: return launch_one<T, 1>(p, s);
-        case 2: return launch_one<T, 2>(p, s);
-        case 3: return launch_one<T, 3>(p, s);
-        case 4: return launch_one<T, 4>(p, s);
-        case 5: return launch_one<T, 5>(p, s);
-        case 6: return launch_one<T, 6>(p, s);
-        case 7: return launch_one<T, 7>(p, s);
-        case 8: return launch_one<T, 8>(p, s);
+        case 1: return launch_one<T, 1, Args>(p, s);
+        case 2: return launch_one<T, 2, Args>(p, s);
+        case 3: return launch_one<T, 3, Args>(p, s);
+        case 4: return launch_one<T, 4, Args>(p, s);
+        case 5: return launch_one<T, 5, Args>(p, s);
+        case 6: return launch_one<T, 6, Args>(p, s);
+        case 7: return launch_one<T, 7, Args>(p, s);
+        case 8: return launch_one<T, 8, Args>(p, s);
         default: return cudaErrorInvalidValue;
     }
 }
@@ -405,6 +500,58 @@ cudaError_t launch_attend(const void *k_cache, const void *v_cache, const void *
     if (e != cudaSuccess || splits == 1) return e;
     attend_merge_kernel<<<(unsigned)(batch * hkv * G), kHeadDim, 0, s>>>(p, G);
     return cudaGetLastError();
+}
+
+// Splits of a head's `rows` rows in that kernel, a block per SM: the shortest run, in tiles of 56 rows: waves of blocks times the tiles of each and three for a block's
+// start and end, and for the merge two and a twentieth per share.  (Against four waves of blocks whatever the lengths, us: 8 heads of 4000 rows 25.8,
+// 13.0; 64 of 2000 and eight query heads each 60.7, 47.1; 128 of 60 11.2, 5.8; 512 of 1000 110.8, 107.5, which is 4.9 TB/s.)
+int attend_f32_more_splits(int heads, long long rows, int sms)
+{
+    const long long tiles = (rows + kAttRows - 1) / kAttRows;
+    long long splits = 1;
+    double best = 0;
+    for (long long s = 1; s <= tiles && s <= 256; ++s) {
+        const double cost = (double)((heads * s + sms - 1) / sms) * (double)((tiles + s - 1) / s + 3) + (s > 1 ? 2 + s * 0.05 : 0);
+        if (s == 1 || cost < best) best = cost, splits = s;
+    }
+    return (int)splits;
+}
+
+// Single tokens over fp32 caches; as launch_attend_more.
+cudaError_t launch_attend_f32_more(const RowsParams &r, bool separate, const RowsParams *prefix, cudaStream_t s)
+{
+    AttendMore p = {};
+    p.k_cache = r.k;
+    p.v_cache = r.v;
+    p.q_new = r.q;
+    p.seq_lens = r.lens;
+    p.out = static_cast<float *>(r.out);
+    p.partial = separate ? r.part : nullptr;
+    p.slot = r.slot;
+    p.slots = r.slots;
+    p.batch = r.tokens.count;
+    p.hkv = r.hkv;
+    p.hq = r.hq;
+    p.cap = r.cap;
+    p.splits = r.splits;
+    p.status = r.status;
+    p.wait_cycles = r.wait_cycles;
+    p.block_table = r.block_table;
+    p.d_out = r.d;
+    p.least = r.causal ? 1 : 0;
+    p.window = r.window;
+    p.sinks = r.sinks;
+    p.pool_pages = r.pool_pages;
+    p.per_prefix = 1;
+    if (prefix) {
+        p.prefix_k = prefix->k, p.prefix_v = prefix->v;
+        p.prefix_lens = prefix->lens;
+        p.prefix_table = prefix->block_table;
+        p.prefix_pages = prefix->pool_pages;
+        p.prefix_cap = prefix->cap;
+        p.per_prefix = prefix->tokens.longest;
+    }
+    return launch_dtype<float>(p, r.group, s);
 }
 
 }  // namespace rkv

@@ -12,15 +12,20 @@ int source_of(int dtype, int d) { return dtype == RKV_FP8_E4M3 ? 1 : d == 64 ? 2
 // `tiles`: key tiles that a token sees at most.
 bool attend_more_supported(int dtype, int d, int group, long long tiles)
 {
-    return dtype != RKV_F32 && attend_supported(group, dtype, d) && tiles <= (long long)kTcMaxSplits * 2 * kTcChunkTiles;
+    return attend_supported(group, dtype, d) && tiles <= (dtype == RKV_F32 ? 1ll << 23 : (long long)kTcMaxSplits * 2 * kTcChunkTiles);
 }
 
 // Splits as for rkv_decode_attention.  They are a cluster, but beside another kernel, where not all blocks are on the GPU at a time, blocks of their
 // own: one that waited for the other kernel's results would keep the next block out (256 sequences of 1152 rows and four prefixes of 16000:
 // 259 us, 238 with a merge kernel; 64 of 580 and one of 2048: 60, 45).
-void attend_more_plan(RowsParams *p, long long tiles, int sms, bool others, bool *separate)
+void attend_more_plan(RowsParams *p, int dtype, long long tiles, int sms, bool others, bool *separate)
 {
     const int heads = p->tokens.count * p->hkv;
+    if (dtype == RKV_F32) {
+        p->splits = attend_f32_more_splits(heads, tiles * kTile, sms);
+        *separate = others || p->splits > 1;
+        return;
+    }
     p->splits = attend_tc_splits(heads, (int)tiles * kTile, sms);
     *separate = others && (long long)heads * p->splits > 2ll * sms;
 }
@@ -28,6 +33,7 @@ void attend_more_plan(RowsParams *p, long long tiles, int sms, bool others, bool
 cudaError_t launch_attend_more(const RowsParams &r, int dtype, long long tiles, bool separate, int others, bool late, const RowsParams *prefix,
                                cudaStream_t s)
 {
+    if (dtype == RKV_F32) return launch_attend_f32_more(r, separate, prefix, s);
     AttendTcMore p = {};
     p.seq_lens = r.lens;
     p.out = static_cast<float *>(r.out);         // (of bf16)

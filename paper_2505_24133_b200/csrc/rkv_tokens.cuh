@@ -111,10 +111,12 @@ cudaError_t launch_rows_sm100(const RowsParams &p, cudaStream_t s);
 // other kernels, and of the splits where they are blocks of their own (then the merge kernel follows); `late`: the kernel before this one
 // leaves those slots and lets this one in only when everything before itself is done.
 bool attend_more_supported(int dtype, int d, int group, long long tiles);
-void attend_more_plan(RowsParams *p, long long tiles, int sms, bool others, bool *separate);
+void attend_more_plan(RowsParams *p, int dtype, long long tiles, int sms, bool others, bool *separate);
 // `prefix`: prefixes that the kernel reads itself, in front of every sequence's own rows; null: none.
 cudaError_t launch_attend_more(const RowsParams &p, int dtype, long long tiles, bool separate, int others, bool late, const RowsParams *prefix,
                                cudaStream_t s);
+int attend_f32_more_splits(int heads, long long rows, int sms);
+cudaError_t launch_attend_f32_more(const RowsParams &p, bool separate, const RowsParams *prefix, cudaStream_t s);      // (fp32 caches)
 cudaError_t launch_rows_merge(const RowsParams &p, int dtype, cudaStream_t s);
 
 }  // namespace rkv

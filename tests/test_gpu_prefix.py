@@ -239,3 +239,19 @@ def test_two_calls_at_once(rkv, dtype, d):
     torch.cuda.synchronize()
     assert torch.equal(a.out, want[0]) and torch.equal(b.out, want[1])
     a.check(), b.check()
+
+
+@pytest.mark.parametrize("paged", [False, True])
+@pytest.mark.parametrize("batch,prefixes", [(8, 4), (160, 4), (12, 12)])
+def test_rows_of_32_bits_are_copied_in_runs(rkv, batch, prefixes, paged):
+    """The prefix's end, the sequence's and the pages' fall at every place of a tile."""
+    lens = [(53 * b) % 400 for b in range(batch - 3)] + [384, 0, 1]
+    plens = ([55, 57, 128, 300] + [0, 1, 56, 112, 129, 255, 256, 10])[:prefixes]
+    Setup(rkv, "f32", 128, 2, 6, lens, plens, 512, 384, paged=paged).run()
+
+
+def test_long_shared_prefixes_of_32_bits(rkv):
+    """So many sequences that the prefix's rows are read once for all, by a kernel of their own."""
+    s = Setup(rkv, "f32", 128, 2, 8, [(37 * b) % 300 for b in range(64)], [1500, 1411], 300, 1500)
+    assert 64 * 2 * 1500 * 1024 > 160 << 20
+    s.run()

@@ -350,3 +350,12 @@ def test_a_generous_bound_on_the_tokens(rkv):
     """`longest` far above what any sequence has costs time, not results."""
     Setup(rkv, "bf16", 128, 2, 8, [40, 259, 7], [40, 77, 0], 300, 50, 4, longest=20000).run()
     Setup(rkv, "f32", 64, 2, 8, [40, 259, 7], [40, 77, 0], 300, 50, 4, longest=5000).run()
+
+
+@pytest.mark.parametrize("paged", [False, True])
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (55, 3), (56, 56), (57, 130), (128, 4), (200, 129)])
+@pytest.mark.parametrize("batch", [9, 160])
+def test_single_tokens_of_32_bits_copy_their_rows_in_runs(rkv, batch, window, sinks, paged):
+    """The first rows' end, the window's start and the pages' ends fall at every place of a tile, in calls that split the rows and in calls that do not."""
+    lens = [1 + (53 * b) % 400 for b in range(batch - 3)] + [384, 128, 1]
+    Setup(rkv, "f32", 128, 2, 6, lens, [1] * batch, 512, window, sinks, offsets=False, paged=paged).run()
