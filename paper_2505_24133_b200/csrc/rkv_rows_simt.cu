@@ -4,6 +4,8 @@
 // at a time, with the running maximum and sum of the softmax; the weighted sum stays in registers.  256 threads as 16 x 16: a thread owns
 // 4 x 4 scores (1 x 4), then 4 rows (1) x d / 16 columns of the output; the 16 threads that share rows are half a warp, so that the weights
 // change hands within the warp.  Bound by fp32 FMAs and the shared-memory reads that feed them (8 vectors per 64 FMAs of the scores; 5 per 16).
+#include <algorithm>
+
 #include "rkv_tokens.cuh"
 
 namespace rkv {
@@ -303,8 +305,19 @@ cudaError_t launch_simt_type(const RowsParams &p, cudaStream_t s)
 
 }  // namespace
 
-// Query rows of a block (16 fp32 single tokens, four heads each, window 1024: 195 us with 64, 114 with 16).
-int rows_simt_rows(const RowsParams &p) { return (long long)p.tokens.longest * p.group <= 16 ? 16 : 64; }
+// Query rows of a block: 16 where the problems have no more, or where tiles of 64 and all splits of the keys would leave most of the SMs idle.
+// (Four heads a token, us with 64, 16.  16 single tokens of window 1024: 195, 114.  64 dimensions, tiles of 64 rows x key tiles: 8 sequences behind 300
+// rows, 24, 45.1, 31.1; 32 behind 330, 48, 72.3, 36.9; 64 behind 150, 64, 66.6, 51.1; 16 behind 2000, 128, 38.9, 41.3; 64 behind 1000, 256, 51.3, 75.0.
+// A prompt of 64 tokens, 32, 23.9, 14.9; of 200, 208, 42.0, 58.1.)
+int rows_simt_rows(const RowsParams &p)
+{
+    const long long rows = (long long)p.tokens.longest * p.group;
+    if (rows <= 16) return 16;
+    long long keys = p.cap;
+    if (p.causal && p.window > 0) keys = std::min(keys, (long long)p.window + p.sinks + p.tokens.longest);
+    const double pairs = (double)((rows + 63) / 64) * p.hkv * p.tokens.count * (double)((keys + kTile - 1) / kTile);
+    return pairs <= 64 ? 16 : 64;
+}
 
 cudaError_t launch_rows_simt(const RowsParams &p, int dtype, cudaStream_t s)
 {
