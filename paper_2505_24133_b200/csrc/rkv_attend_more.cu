@@ -1,4 +1,5 @@
-// Decode-step attention on the tensor cores (rkv_attend_tc.cuh) for single tokens that see part of their cache, or a shared prefix as well.
+// Decode-step attention for single tokens that see part of their cache, or a shared prefix as well: on the tensor cores (rkv_attend_tc.cuh), and for
+// fp32 caches rkv_attend.cu.
 #include "rkv_attend_tc.cuh"
 
 namespace rkv {

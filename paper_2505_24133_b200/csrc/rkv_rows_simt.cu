@@ -1,6 +1,6 @@
 // Attention of many query rows over a cache, CUDA-core form (fp32 products), and the merge of partial results.
 //
-// A block takes 64 query rows (16 where a problem has no more) of one (problem, KV head) and goes once over its share of the key tiles, 64 keys
+// A block takes 64 query rows (or 16: see rows_simt_rows) of one (problem, KV head) and goes once over its share of the key tiles, 64 keys
 // at a time, with the running maximum and sum of the softmax; the weighted sum stays in registers.  256 threads as 16 x 16: a thread owns
 // 4 x 4 scores (1 x 4), then 4 rows (1) x d / 16 columns of the output; the 16 threads that share rows are half a warp, so that the weights
 // change hands within the warp.  Bound by fp32 FMAs and the shared-memory reads that feed them (8 vectors per 64 FMAs of the scores; 5 per 16).
