@@ -47,8 +47,9 @@ struct RowsShape {
                          kNextFree = kNext + 2, kBars = kNextFree + 2;                     // kNextFree[2]: every warp has read it
     static constexpr int kOffMisc = kOffBars + kBars * 8;
     static constexpr int kOffNext = (kOffMisc + 16 + 15) / 16 * 16;      // two answers of 16 bytes
-    static constexpr int kOffMost = kOffNext + 32;      // [tiles][2 halves][128]: the rows' largest scores, then as many sums
-    static constexpr int kSmem = kOffMost + 2 * kTiles * 256 * 4 + 1024;
+    static constexpr int kOffMost = kOffNext + 32;      // [tiles][2 key tiles in turn][2 halves][128]: the rows' largest scores
+    static constexpr int kOffSums = kOffMost + kTiles * 512 * 4;         // [tiles][2 halves][128]: the rows' sums of weights
+    static constexpr int kSmem = kOffSums + kTiles * 256 * 4 + 1024;
     static constexpr int kThreads = kTiles * 256 + 64;
     static constexpr uint32_t kCols = kTiles == 2 ? 512 : 256;
     // tensor memory: scores, weights, outputs; one row tile: the weights of each half of the keys over its scores
@@ -449,7 +450,7 @@ rows_tc_kernel(RowsParams p, int tokens_per_tile, int pieces, int items, const _
         const int r = warp >> 3, half = (warp >> 2) & 1, row = threadIdx.x & 127;        // row tile, keys 64 half .., row (= lane of tensor memory)
         const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         const uint32_t s_col = lanes + 64 * half, w_col = lanes + S::kWeightCol(r, half), o_col = lanes + S::kOutCol(r) + half * (kDim / 2);
-        float *mosts = reinterpret_cast<float *>(smem + S::kOffMost) + r * 256;
+        float *mosts = reinterpret_cast<float *>(smem + S::kOffMost) + r * 512, *sums = reinterpret_cast<float *>(smem + S::kOffSums) + r * 256;
         auto pair_sync = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(1 + r * 4 + (warp & 3)) : "memory"); };       // the two warps of 32 rows
         const float c2 = 1.4426950408889634f * rsqrtf((float)kDim);
         int steps = 0;                                                   // key tiles so far
@@ -512,10 +513,13 @@ rows_tc_kernel(RowsParams p, int tokens_per_tile, int pieces, int items, const _
                     for (int e = 2; e < 16; e += 2) top[i] = max3(top[i], __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
                 }
                 float most = max3(fmaxf(top[0], top[1]), top[2], top[3]);
-                // (written again with the next scores, which come when all threads have handed in these weights)
-                mosts[half * 128 + row] = most;
+                // Two buffers in turn: a thread writes one again two key tiles later, behind the pair's next barrier, which the other thread comes to
+                // when it has read this.  (With one, nothing but time would lie between that read and the next write: of two row tiles the next
+                // scores are formed as soon as these are in registers.)
+                float *now = mosts + ((steps + j) & 1) * 256;
+                now[half * 128 + row] = most;
                 pair_sync();
-                most = fmaxf(most, mosts[(half ^ 1) * 128 + row]);
+                most = fmaxf(most, now[(half ^ 1) * 128 + row]);
                 const bool outgrown = (most - m) * c2 > kSlack || (m == -INFINITY && most > -INFINITY);
                 if (__any_sync(0xffffffffu, outgrown)) {
                     const float next = outgrown ? most : m, shrink = outgrown ? exp2f((m - next) * c2) : 1.f;
@@ -571,7 +575,6 @@ rows_tc_kernel(RowsParams p, int tokens_per_tile, int pieces, int items, const _
             if (ok && T > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar(S::kOut + r), (steps - 1) & 1, abort_flag, sink));
             tc_fence_after();
             if (T > 0) {                                                     // (the other thread comes to the next item's when it has read these)
-                float *sums = mosts + kTiles * 256;
                 sums[half * 128 + row] = l;
                 pair_sync();
                 l += sums[(half ^ 1) * 128 + row];

@@ -359,3 +359,31 @@ def test_single_tokens_of_32_bits_copy_their_rows_in_runs(rkv, batch, window, si
     """The first rows' end, the window's start and the pages' ends fall at every place of a tile, in calls that split the rows and in calls that do not."""
     lens = [1 + (53 * b) % 400 for b in range(batch - 3)] + [384, 128, 1]
     Setup(rkv, "f32", 128, 2, 6, lens, [1] * batch, 512, window, sinks, offsets=False, paged=paged).run()
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("fp8", 128)])
+@pytest.mark.parametrize("G,new", [(4, [1500, 900]), (7, [1100, 1033]), (4, [20, 11])])
+def test_maxima_that_move_between_the_halves_of_a_tile(rkv, dtype, d, G, new):
+    """Keys whose size changes every 64 rows: the maximum is now in one thread's half of a row's keys, now in the other's, and each has to take
+    it from the other at every tile.  The same to the bit whenever it is called."""
+    s = Setup(rkv, dtype, d, 2, 2 * G, [1500, 1100], new, 1536, 0, 0)
+    size = torch.tensor([0.25, 1.0, 2.0, 0.5, 0.25, 2.0, 1.0], device="cuda")[torch.arange(1536, device="cuda") // 64 % 7]
+    for x in (s.k, s.k0):
+        x.copy_((x.float() * size[:, None]).to(x.dtype))
+    assert s.call() == 0
+    torch.cuda.synchronize()
+    first = 0
+    for b, (L, n) in enumerate(zip(s.lens, s.new)):
+        for h in range(s.hkv):
+            heads = slice(h * G, (h + 1) * G)
+            ref, mean = attention(s.q[first:first + n, heads], s.k0[b, h, :L], s.v0[b, h, :L], visible(L, n, 0, 0))
+            # keys up to twice as long as those that attention_tolerance counts on: its scores' part once more
+            tol = attention_tolerance(ref, mean, L, d, s.out.dtype) + mean * 2 * (d + 2) * 2.0 ** -24 * 2 * d ** 0.5
+            assert ((s.out[first:first + n, heads].double() - ref).abs() <= tol).all()
+        first += n
+    want = s.out.clone()
+    for _ in range(30):
+        s.out.zero_()
+        assert s.call() == 0
+        torch.cuda.synchronize()
+        assert torch.equal(s.out, want)
