@@ -18,7 +18,8 @@ bool attend_more_supported(int dtype, int d, int group, long long tiles)
 
 // Splits as for rkv_decode_attention.  They are a cluster, but beside another kernel, where not all blocks are on the GPU at a time, blocks of their
 // own: one that waited for the other kernel's results would keep the next block out (256 sequences of 1152 rows and four prefixes of 16000:
-// 259 us, 238 with a merge kernel; 64 of 580 and one of 2048: 60, 45).
+// 259 us, 238 with a merge kernel; 64 of 580 and one of 2048: 60, 45).  Nor are they where the keys of many heads go to more blocks than a cluster
+// has (from 241 tiles on; 128 heads of 32768 rows, 18 shares each: 307 us, 7.0 TB/s, of 8-bit caches 166 us).
 void attend_more_plan(RowsParams *p, int dtype, long long tiles, int sms, bool others, bool *separate)
 {
     const int heads = p->tokens.count * p->hkv;
@@ -28,7 +29,7 @@ void attend_more_plan(RowsParams *p, int dtype, long long tiles, int sms, bool o
         return;
     }
     p->splits = attend_tc_splits(heads, (int)tiles * kTile, sms);
-    *separate = others && (long long)heads * p->splits > 2ll * sms;
+    *separate = p->splits > kTcMaxSplits || (others && (long long)heads * p->splits > 2ll * sms);
 }
 
 cudaError_t launch_attend_more(const RowsParams &r, int dtype, long long tiles, bool separate, int others, bool late, const RowsParams *prefix,

@@ -255,3 +255,35 @@ def test_long_shared_prefixes_of_32_bits(rkv):
     s = Setup(rkv, "f32", 128, 2, 8, [(37 * b) % 300 for b in range(64)], [1500, 1411], 300, 1500)
     assert 64 * 2 * 1500 * 1024 > 160 << 20
     s.run()
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("fp8", 128)])
+def test_prefixes_in_front_of_long_caches_of_many_heads(rkv, dtype, d):
+    """A prefix for each sequence, read by the blocks that read its own rows; more of them to a head than a cluster has."""
+    from test_gpu_window import shared_pages
+    gen, B, hkv, G, cap, rows = torch.Generator(device="cuda").manual_seed(62), 9, 8, 2, 20480, 10368
+    k, v, table = shared_pages(dtype, d, B * hkv, cap + rows, gen)
+    own, shared = table[:, :cap // 128].contiguous(), table[:, cap // 128:].contiguous().view(B, hkv, rows // 128)
+    lens, plens = [cap, 0, cap - 77, 200, 1, 15000, 129, cap, 0], [rows, rows - 1, 300, 0, rows, 128, 1, 5000, 0]
+    seq, pseq = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in (lens, plens))
+    q = torch.randn(B, hkv * G, d, generator=gen, device="cuda").to(WIDE[dtype])
+    out, status = torch.full_like(q, 7.0), torch.zeros(1, dtype=torch.int32, device="cuda")
+    desc = descriptor(rkv, B, hkv, hkv * G, d, dtype, status, own, k.shape[0])
+    prefix = rkv.rkv_prefix(k, v, pseq, shared)
+    n = rkv.rkv_prefix_workspace_bytes(desc, cap - 1, 1, prefix)
+    room = torch.full((max(n, 256),), 0xFF, dtype=torch.uint8, device="cuda")
+    desc.workspace, desc.workspace_bytes = room.data_ptr(), n
+    assert rkv.rkv_prefix_attention(desc, k, v, q, seq, out, cap - 1, 1, prefix) == 0
+    torch.cuda.synchronize()
+    assert int(status.item()) == 0
+    for b, (L, P) in enumerate(zip(lens, plens)):
+        for h in range(hkv):
+            heads = slice(h * G, (h + 1) * G)
+            if L + P == 0:
+                assert (out[b, heads] == 0).all()
+                continue
+            keys, values = (torch.cat([x[shared[b, h].long()].float().view(rows, d)[:P], x[own[b * hkv + h].long()].float().view(cap, d)[:L]])
+                            for x in (k, v))
+            ref, size = attention(q[b:b + 1, heads], keys, values, torch.ones(1, P + L, dtype=torch.bool, device="cuda"))
+            over = (out[b:b + 1, heads].double() - ref).abs() - attention_tolerance(ref, size, P + L, d, q.dtype)
+            assert float(over.max()) <= 0, (b, h)

@@ -387,3 +387,38 @@ def test_maxima_that_move_between_the_halves_of_a_tile(rkv, dtype, d, G, new):
         assert s.call() == 0
         torch.cuda.synchronize()
         assert torch.equal(s.out, want)
+
+
+def shared_pages(dtype, d, heads, cap, gen, pages=500):
+    """Pools of pages that all heads' tables draw from, so that long caches of many heads take little room: pool of K, of V, table [heads, cap / 128]."""
+    pools = [torch.randn(pages, 128, d, generator=gen, device="cuda").to(TYPES[dtype]) for _ in range(2)]
+    table = torch.stack([torch.randperm(pages, generator=gen, device="cuda")[:cap // 128] for _ in range(heads)])
+    return pools[0], pools[1], table.to(torch.int32)
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("fp8", 128), ("f32", 128), ("fp8", 64)])
+@pytest.mark.parametrize("B,cap,window,sinks", [(9, 30848, 0, 0), (5, 57344, 0, 0), (8, 57344, 35000, 200)])
+def test_single_tokens_over_long_caches_of_many_heads(rkv, dtype, d, B, cap, window, sinks):
+    """The keys of a head are split between more blocks than a cluster has."""
+    gen, hkv, G = torch.Generator(device="cuda").manual_seed(61), 8, 2
+    k, v, table = shared_pages(dtype, d, B * hkv, cap, gen)
+    lens = [cap, 1, cap - 77, 200, cap - 128, 15000, 129, cap, 128][:B]
+    seq = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    q = torch.randn(B, hkv * G, d, generator=gen, device="cuda").to(WIDE[dtype])
+    out, status = torch.full_like(q, 7.0), torch.zeros(1, dtype=torch.int32, device="cuda")
+    desc = descriptor(rkv, B, hkv, hkv * G, d, dtype, status, table, k.shape[0])
+    tokens = rkv.rkv_tokens(B, 1)
+    n = rkv.rkv_window_workspace_bytes(desc, cap - 1, 1, tokens, window, sinks)
+    room = torch.full((max(n, 256),), 0xFF, dtype=torch.uint8, device="cuda")
+    desc.workspace, desc.workspace_bytes = room.data_ptr(), n
+    assert rkv.rkv_window_attention(desc, k, v, q, seq, out, cap - 1, 1, tokens, window, sinks) == 0
+    torch.cuda.synchronize()
+    assert int(status.item()) == 0
+    for b, L in enumerate(lens):
+        seen = visible(L, 1, window, sinks)
+        for h in range(hkv):
+            rows = table[b * hkv + h].long()
+            keys, values = (x[rows].float().view(cap, d)[:L] for x in (k, v))
+            ref, size = attention(q[b:b + 1, h * G:(h + 1) * G], keys, values, seen)
+            over = (out[b:b + 1, h * G:(h + 1) * G].double() - ref).abs() - attention_tolerance(ref, size, L, d, q.dtype)
+            assert float(over.max()) <= 0, (b, h)

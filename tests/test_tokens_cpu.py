@@ -132,3 +132,16 @@ def test_workspace_sizes(rkv):
     assert rkv.rkv_window_workspace_bytes(_desc(rkv, batch=512), 1000, 1, rkv.rkv_tokens(512 * 64, 64), 0, 0) == 0
     x = rkv.RkvPrefix(GOOD, GOOD, 2, 100000, GOOD, None, 0)
     assert rkv.rkv_prefix_workspace_bytes(d, 1000, 1, x) > 0 and rkv.rkv_prefix_workspace_bytes(_desc(rkv, batch=3), 1000, 1, x) == 0
+
+
+@pytest.mark.parametrize("dtype,d", [("RKV_BF16", 128), ("RKV_BF16", 64), ("RKV_FP8_E4M3", 128)])
+@pytest.mark.parametrize("batch,cap,window", [(16, 32768, 0), (8, 40960, 0), (9, 30848, 0), (5, 57344, 0), (8, 1 << 20, 35000)])
+def test_more_shares_than_a_cluster_has_blocks_have_room(rkv, dtype, d, batch, cap, window):
+    """Single tokens of many heads over so many rows that a head's keys go to more than 16 blocks, the most of a cluster: the blocks' partial
+    results have a place in the workspace."""
+    desc = _desc(rkv, batch=batch, dtype=getattr(rkv, dtype), head_dim=d, block_table=GOOD, pool_pages=9)
+    tokens = rkv.rkv_tokens(batch, 1)
+    assert rkv.rkv_window_workspace_bytes(desc, cap - 128, 128, tokens, window, 0) >= batch * 32 * 17 * (d + 4) * 4
+    x = rkv.RkvPrefix(GOOD, GOOD, batch, 128, GOOD, GOOD, 9)         # a short prefix for each, read by the same blocks
+    if window == 0 and cap < 57344:
+        assert rkv.rkv_prefix_workspace_bytes(desc, cap - 128, 128, x) >= batch * 32 * 17 * (d + 4) * 4
