@@ -36,10 +36,14 @@
 //
 // 8-bit caches, as they are stored (kCodes, the calls of AttendTcMore): with bf16 operands the chain widen -> product of a block bounds the
 // call at 4 TB/s, so here both products take the codes themselves (kind::f8f6f4; products of codes are exact, the accumulators fp32), and the other
-// operands come in two E4M3 parts each, hi and 16 times what hi left, in the rows g and 8 + g that the bf16 weights' two parts take.  A query row
-// is scaled by a power of two to a largest element in [128, 256): two parts of four bits hold a bf16 number exactly, elements below 2^-13 of
-// the largest to 2^-21 of it.  A weight times 256 is held to 2^-8 of itself, as one bf16 part would hold it (to 2^-22 in all where that
-// is more); the sum of the weights is taken from the parts.
+// operands come in parts that add up to them.  A query row is scaled by a power of two to a largest element in [128, 256) and has two E4M3 parts, hi
+// and 16 times what hi left, in the rows g and 8 + g that the bf16 weights' two parts take: four bits each hold a bf16 number exactly, elements below
+// 2^-13 of the largest to 2^-21 of it, which moves a score by less than its fp32 sum may be off by.  A weight times 2^15 is rounded to fp16 (2^-11 of
+// itself down to 2^-29, 2^-40 below) and that is held exactly in four E5M2 parts, each the upper byte of 8 times what the one before left, in the
+// rows g, 8 + g, 16 + g and 24 + g (N = 32); the sum of the weights is taken from the fp16 numbers.  (Two E4M3 parts lose weights below 2^-22, and with them
+// the whole output where a row whose values are small has nearly all of the weight.  64 sequences x 8 heads of 4224 rows, two parts and these: four queries
+// to a head 102.0 us, 102.3; eight 116, 124.)
+// The output's 32 columns lie over score columns that have been read: tile 0's, and of a second chunk tiles 0's and 1's.
 //
 // Of 64 dimensions, as they are stored (kHalf, the calls of AttendTcMore): the tiles go to the tensor cores as they land, too, keys as four steps of 16
 // columns, values as the lower half of M.
@@ -77,8 +81,9 @@ constexpr int kOffRaw = kConvBufs * kTcTileBytes;    // then kRawStages raw stag
 constexpr int kRawBytes = kTile * kHeadDim;          // a tile of E4M3 codes
 constexpr int kOffQ = kOffRing + kTcStages * kTcTileBytes;
 static_assert(kOffRaw + kRawStages * kRawBytes <= kOffQ, "the 8-bit layout fits the room of the ring");
-constexpr int kOffP = kOffQ + kTcSmall;              // two buffers
-constexpr int kOffCodeQ = kOffP + kTcSmall / 2;       // [16 x 128] codes: 2 KB each, the queries' parts behind the first buffer's weights
+constexpr float kCodeWeight = 32768.f;               // kCodes: what the weights are multiplied by
+// two buffers.  kCodes: [32 x 128] codes each; the queries' parts, [16 x 128] codes, take the queries' place
+constexpr int kOffP = kOffQ + kTcSmall;
 constexpr int kOffRed = kOffP + 2 * kTcSmall;        // [4 warps][8] floats: reductions over the softmax threads
 constexpr int kOffBars = kOffRed + 4 * 8 * 4;
 enum {
@@ -170,14 +175,10 @@ __device__ __forceinline__ uint32_t small_off(int g, int k)
 // The same for a [16 x 128] operand of codes: rows of 128 bytes.
 __device__ __forceinline__ uint32_t code_off(int g, int k) { return (uint32_t)(g * 128 + (((k >> 4) ^ (g & 7)) << 4) + (k & 15)); }
 // x as hi + lo / 16 in two codes
-__device__ __forceinline__ void two_codes(float x, uint8_t *hi, uint8_t *lo, float *value)
+__device__ __forceinline__ void two_codes(float x, uint8_t *hi, uint8_t *lo)
 {
-    const __nv_fp8_storage_t h = __nv_cvt_float_to_fp8(x, __NV_SATFINITE, __NV_E4M3);
-    const float hf = __half2float(__half(__nv_cvt_fp8_to_halfraw(h, __NV_E4M3)));
-    const __nv_fp8_storage_t l = __nv_cvt_float_to_fp8((x - hf) * 16.f, __NV_SATFINITE, __NV_E4M3);
-    *hi = h;
-    *lo = l;
-    *value = hf + __half2float(__half(__nv_cvt_fp8_to_halfraw(l, __NV_E4M3))) * 0.0625f;
+    *hi = __nv_cvt_float_to_fp8(x, __NV_SATFINITE, __NV_E4M3);
+    *lo = __nv_cvt_float_to_fp8((x - __half2float(__half(__nv_cvt_fp8_to_halfraw(*hi, __NV_E4M3)))) * 16.f, __NV_SATFINITE, __NV_E4M3);
 }
 __device__ __forceinline__ void umma_codes(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accum)
 {
@@ -448,7 +449,7 @@ attend_tc_kernel(Args p, const __grid_constant__ MapsFor<Args> maps)
                     if (kHalf)
                         umma_tile_k64(tmem + 16 * (chunks + t), sbase + kOffRing + s * kRawBytes, sbase + kOffQ, idesc_s);
                     else if (kCodes)
-                        umma_tile_row128<true>(tmem + 16 * (chunks + t), sbase + kOffRing + s * kRawBytes, sbase + kOffCodeQ, idesc_s);
+                        umma_tile_row128<true>(tmem + 16 * (chunks + t), sbase + kOffRing + s * kRawBytes, sbase + kOffQ, idesc_s);
                     else
                         umma_tile_k128_halves(tmem + 16 * (chunks + t), sbase + kOffRing + s * kTcTileBytes, kTcHalf, sbase + kOffQ,
                                           kTcSmall / 2, idesc_s);
@@ -459,14 +460,16 @@ attend_tc_kernel(Args p, const __grid_constant__ MapsFor<Args> maps)
                     const int s = i % kBufs, pt = done + t, pb = pt & 1;
                     ok = mbar_wait(bar(kRingFull + s), (i / kBufs) & 1, abort_flag, sink) &&
                          mbar_wait(bar(kBarPFull + pb), (pt >> 1) & 1, abort_flag, sink);
+                    // (the second chunk's output lies over the scores of its first two tiles, the first's over those of its first at most)
+                    if (kCodes && kForm == kTwo && c && t == 0 && ok) ok = mbar_wait(bar(kBarPFull + (pb ^ 1)), ((pt + 1) >> 1) & 1, abort_flag, sink);
                     if (!ok) break;
                     tc_fence_after();
                     if (kCodes) {
 #pragma unroll
                         for (int ks = 0; ks < 4; ++ks) {     // 32 keys per step
                             const uint32_t a_addr = sbase + kOffRing + s * kRawBytes + ks * 4096, b_addr = sbase + kOffP + pb * kTcSmall + ks * 32;
-                            // A: the 128 dimensions are one atom along M, 8-row groups along K 1 KB apart
-                            umma_codes(tmem + 16 * c, smem_desc(a_addr), smem_desc(b_addr), instr_desc_codes(kTile, 16) | (1u << 15),
+                            // A: E4M3, B: E5M2; the 128 dimensions are one atom along M, 8-row groups along K 1 KB apart
+                            umma_codes(tmem + 32 * c, smem_desc(a_addr), smem_desc(b_addr), instr_desc_codes(kTile, 32) | (1u << 10) | (1u << 15),
                                        (t > 0 || ks > 0) ? 1u : 0u);
                         }
                         umma_commit(bar(kRingEmpty + s));
@@ -543,13 +546,13 @@ attend_tc_kernel(Args p, const __grid_constant__ MapsFor<Args> maps)
             // 2^(134 - exponent field) puts the largest into [128, 256); a row of zeros, or of numbers under 2^-100, by 2^100 at most
             const int up = min(max(134 - (int)(__float_as_uint(most) >> 23), -100), 100);
             const float scale = __uint_as_float((uint32_t)(127 + up) << 23);
+            softmax_sync();                              // the codes take the queries' place
             if (g < G) {
                 uint8_t hi[8], lo[8];
-                float value;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) two_codes(f[e] * scale, hi + e, lo + e, &value);
-                *reinterpret_cast<uint2 *>(smem + kOffCodeQ + code_off(g, k0)) = make_uint2(hi[0] | hi[1] << 8 | hi[2] << 16 | (uint32_t)hi[3] << 24, hi[4] | hi[5] << 8 | hi[6] << 16 | (uint32_t)hi[7] << 24);
-                *reinterpret_cast<uint2 *>(smem + kOffCodeQ + code_off(8 + g, k0)) = make_uint2(lo[0] | lo[1] << 8 | lo[2] << 16 | (uint32_t)lo[3] << 24, lo[4] | lo[5] << 8 | lo[6] << 16 | (uint32_t)lo[7] << 24);
+                for (int e = 0; e < 8; ++e) two_codes(f[e] * scale, hi + e, lo + e);
+                *reinterpret_cast<uint2 *>(smem + kOffQ + code_off(g, k0)) = make_uint2(hi[0] | hi[1] << 8 | hi[2] << 16 | (uint32_t)hi[3] << 24, hi[4] | hi[5] << 8 | hi[6] << 16 | (uint32_t)hi[7] << 24);
+                *reinterpret_cast<uint2 *>(smem + kOffQ + code_off(8 + g, k0)) = make_uint2(lo[0] | lo[1] << 8 | lo[2] << 16 | (uint32_t)lo[3] << 24, lo[4] | lo[5] << 8 | lo[6] << 16 | (uint32_t)lo[7] << 24);
                 if ((r & 15) == 0) red[g] = __uint_as_float((uint32_t)(127 - up) << 23) * c2;
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");       // generic writes -> tensor-core reads
@@ -608,27 +611,35 @@ attend_tc_kernel(Args p, const __grid_constant__ MapsFor<Args> maps)
                 uint32_t acc[16];
                 tmem_ld16(lane_base + 16 * (chunks + t), acc);
                 tmem_wait16(acc);
-                if (kForm == kTwo) tc_fence_before();    // (the second chunk's scores are written behind this thread's arrival below)
+                if (kForm == kTwo || kCodes) tc_fence_before();    // (the second chunk's scores, or outputs, are written behind this thread's arrival below)
                 const bool valid = seen(done + t, r);
                 uint8_t *pt_smem = smem + kOffP + pb * kTcSmall;
+                // (a NaN or infinite score of a row that is not cached never gets here: `valid` decides)
+                auto weight = [&](int g) -> float { return valid ? exp2f(score(acc, g) - m[g]) : 0.f; };
+                if constexpr (kCodes) {
 #pragma unroll
-                for (int g = 0; g < G; ++g) {
-                    // (a NaN or infinite score of a row that is not cached never gets here: `valid` decides)
-                    const float w = valid ? exp2f(score(acc, g) - m[g]) : 0.f;
-                    if constexpr (kCodes) {
-                        uint8_t hi, lo;
-                        float value;
-                        two_codes(w * 256.f, &hi, &lo, &value);
-                        l[g] += value;                   // (of weights times 256, like the products)
-                        pt_smem[code_off(g, r)] = hi;
-                        pt_smem[code_off(8 + g, r)] = lo;
-                        continue;
+                    for (int g = 0; g < G; g += 2) {         // two queries at a time
+                        __half2 left = __floats2half2_rn(weight(g) * kCodeWeight, g + 1 < G ? weight(g + 1) * kCodeWeight : 0.f);
+                        l[g] += __low2float(left);           // (of weights times 2^15, like the products)
+                        if (g + 1 < G) l[g + 1] += __high2float(left);
+#pragma unroll
+                        for (int part = 0; part < 4; ++part) {
+                            const uint32_t bits = *reinterpret_cast<const uint32_t *>(&left) & 0xFF00FF00u;
+                            pt_smem[code_off(g + 8 * part, r)] = (uint8_t)(bits >> 8);
+                            if (g + 1 < G) pt_smem[code_off(g + 1 + 8 * part, r)] = (uint8_t)(bits >> 24);
+                            left = __hmul2(__hsub2(left, *reinterpret_cast<const __half2 *>(&bits)), __float2half2_rn(8.f));
+                        }
                     }
-                    const __nv_bfloat16 hi = __float2bfloat16_rn(w);
-                    const __nv_bfloat16 lo = __float2bfloat16_rn(w - __bfloat162float(hi));
-                    l[g] += __bfloat162float(hi) + __bfloat162float(lo);
-                    *reinterpret_cast<__nv_bfloat16 *>(pt_smem + small_off(g, r)) = hi;
-                    *reinterpret_cast<__nv_bfloat16 *>(pt_smem + small_off(8 + g, r)) = lo;
+                } else {
+#pragma unroll
+                    for (int g = 0; g < G; ++g) {
+                        const float w = weight(g);
+                        const __nv_bfloat16 hi = __float2bfloat16_rn(w);
+                        const __nv_bfloat16 lo = __float2bfloat16_rn(w - __bfloat162float(hi));
+                        l[g] += __bfloat162float(hi) + __bfloat162float(lo);
+                        *reinterpret_cast<__nv_bfloat16 *>(pt_smem + small_off(g, r)) = hi;
+                        *reinterpret_cast<__nv_bfloat16 *>(pt_smem + small_off(8 + g, r)) = lo;
+                    }
                 }
                 if (!kFp8 && !valid) {
                     // a row beyond the sequence's length may hold anything, and 0 x NaN would spoil the product: its V row
@@ -668,30 +679,40 @@ attend_tc_kernel(Args p, const __grid_constant__ MapsFor<Args> maps)
         }
         softmax_sync();
         if (ok) ok = mbar_wait(bar(kBarOut), 0, abort_flag, sink);
-        uint32_t o[16], o0[16];
+        // the queries' outputs of this thread's dimension and chunk c, from the columns of the parts
+        constexpr int kOutCols = kCodes ? 32 : 16;
+        constexpr float kLow = kCodes ? 0.125f : 1.f, kScale = kCodes ? 1.f / kCodeWeight : 1.f;
+        float num[G], num0[G];
+        auto outputs = [&](int c, float (&to)[G]) {
+            uint32_t o[16];
+            tmem_ld16(lane_base + kOutCols * c, o);
+            tmem_wait16(o);
 #pragma unroll
-        for (int c = 0; c < 16; ++c) o[c] = o0[c] = 0u;
+            for (int g = 0; g < G; ++g) to[g] = fmaf(__uint_as_float(o[8 + g]), kLow, __uint_as_float(o[g]));
+            if constexpr (kCodes) {
+                tmem_ld16(lane_base + kOutCols * c + 16, o);
+                tmem_wait16(o);
+#pragma unroll
+                for (int g = 0; g < G; ++g) to[g] = fmaf(fmaf(__uint_as_float(o[8 + g]), kLow, __uint_as_float(o[g])), kLow * kLow, to[g]);
+            }
+        };
+#pragma unroll
+        for (int g = 0; g < G; ++g) num[g] = num0[g] = 0.f;
         if (ok) {
             tc_fence_after();
-            tmem_ld16(lane_base + 16 * (chunks - 1), o);
-            tmem_wait16(o);
-            if (chunks > 1) {
-                tmem_ld16(lane_base, o0);
-                tmem_wait16(o0);
-            }
+            outputs(chunks - 1, num);
+            if (chunks > 1) outputs(0, num0);
         }
 #pragma unroll
         for (int g = 0; g < G; ++g) {
             float den = ok ? (red[g] + red[8 + g]) + (red[16 + g] + red[24 + g]) : 0.f;     // error path: zeros
-            constexpr float kLow = kCodes ? 0.0625f : 1.f;    // what the second part counts
-            float num = fmaf(__uint_as_float(o[8 + g]), kLow, __uint_as_float(o[g]));
-            if (chunks > 1) num = fmaf(__uint_as_float(o0[8 + g]), kLow, __uint_as_float(o0[g])) * w0[g] + num * w1[g];
-            if (kCodes) num *= 1.f / 256.f, den *= 1.f / 256.f;
+            if (chunks > 1) num[g] = num0[g] * w0[g] + num[g] * w1[g];
+            num[g] *= kScale, den *= kScale;
             if (r >= kDim) continue;                          // (64 dimensions: the padded half of the output)
             if (!merges) {
-                put(out + (size_t)g * kDim + r, den > 0.f ? num / den : 0.f);
+                put(out + (size_t)g * kDim + r, den > 0.f ? num[g] / den : 0.f);
             } else {
-                part[g * part_stride + r] = num;
+                part[g * part_stride + r] = num[g];
                 if (r == 0) {
                     part[g * part_stride + part_max] = ok ? m[g] : -INFINITY;
                     part[g * part_stride + part_max + 1] = den;

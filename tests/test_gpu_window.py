@@ -422,3 +422,31 @@ def test_single_tokens_over_long_caches_of_many_heads(rkv, dtype, d, B, cap, win
             ref, size = attention(q[b:b + 1, h * G:(h + 1) * G], keys, values, seen)
             over = (out[b:b + 1, h * G:(h + 1) * G].double() - ref).abs() - attention_tolerance(ref, size, L, d, q.dtype)
             assert float(over.max()) <= 0, (b, h)
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("fp8", 128), ("fp8", 64), ("f32", 128)])
+@pytest.mark.parametrize("B,hkv,G,cap", [(3, 2, 4, 128), (2, 1, 8, 640), (40, 8, 1, 1920), (30, 8, 3, 3584)])
+def test_many_small_weights_beside_one_that_counts_for_nothing(rkv, dtype, d, B, hkv, G, cap):
+    """One row takes nearly all the weight, and its values are zeros: the output is made of the weights of all other rows, 2^-8 to 2^-30 of the
+    largest, and each of them is held as well as a large one."""
+    key = lambda x: torch.tensor(x, device="cuda").to(TYPES[dtype])                # noqa: E731
+    for k in (0.5, 0.125, 0.0, -0.125, -0.25, -0.375, -0.5, -0.625, -0.75):          # weights 2^(-1.443 sqrt(d) (1 - k)) of the largest
+        lens = [cap - 28 - b for b in range(B)]
+        s = Setup(rkv, dtype, d, hkv, hkv * G, lens, [1] * B, cap, 0, 0, offsets=False)
+        for x, other in ((s.k, s.v), (s.k0, s.v0)):
+            for b, L in enumerate(lens):
+                x[b, :, :L] = key(k)
+                x[b, :, 5] = key(1.0)
+                other[b, :, :L] = (other[b, :, :L].float() + 1.0).to(other.dtype)
+                other[b, :, 5] = key(0.0)
+        s.q.fill_(1.0)
+        assert s.call() == 0
+        torch.cuda.synchronize()
+        assert int(s.status.item()) == 0
+        for b in {0, B // 2, B - 1}:
+            L = lens[b]
+            for h in range(hkv):
+                ref, size = attention(s.q[b:b + 1, h * G:(h + 1) * G], s.k0[b, h, :L], s.v0[b, h, :L], visible(L, 1, 0, 0))
+                # |q| |k| = d at most, values up to 1 larger: within what attention_tolerance counts on, whose `size` is that of these values
+                over = (s.out[b:b + 1, h * G:(h + 1) * G].double() - ref).abs() - attention_tolerance(ref, size, L, d, s.out.dtype)
+                assert float(over.max()) <= 0, (k, b, h, float((over / size).max()))
