@@ -136,19 +136,30 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b)
         : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return d;
 }
-// 2^x for two x <= 127 without the special-function unit: x = n + f, |f| <= 1/2, by adding and subtracting 3 2^22; 2^f by the polynomial of
-// degree 4 with the smallest relative error (2.7e-6 with fp32 rounding; a weight's own rounding is up to 3.9e-3); n onto the exponent.
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, d;\n\t"
+        "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
+        "mul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+// 2^x for two x <= 127 without the special-function unit: x = n + f, |f| <= 1/2, by adding and subtracting 3 2^22 + 127, whose sum's last bits
+// are the exponent field of 2^n; times 2^f by the polynomial of degree 4 with the smallest relative error (2.7e-6 with fp32 rounding; a weight's
+// own rounding is up to 3.9e-3).  From -126.5 down the field is 0 and so is the result: hidden keys, whose scores are -inf, count for nothing,
+// whatever their values are.
 __device__ __forceinline__ float2 exp2_poly(float2 x)
 {
-    x = make_float2(fmaxf(x.x, -126.f), fmaxf(x.y, -126.f));             // (from there down the weights are 0 for all that they do)
-    const float2 big = make_float2(12582912.f, 12582912.f), t = add2(x, big);
+    x = make_float2(fmaxf(x.x, -127.f), fmaxf(x.y, -127.f));
+    const float2 big = make_float2(12583039.f, 12583039.f), t = add2(x, big);
     const float2 f = add2(x, fma2(t, make_float2(-1.f, -1.f), big));
     float2 y = fma2(make_float2(0.009570101276040077f, 0.009570101276040077f), f, make_float2(0.05591785907745361f, 0.05591785907745361f));
     y = fma2(y, f, make_float2(0.240247443318367f, 0.240247443318367f));
     y = fma2(y, f, make_float2(0.6931217908859253f, 0.6931217908859253f));
     y = fma2(y, f, make_float2(0.9999992847442627f, 0.9999992847442627f));
-    return make_float2(__uint_as_float(__float_as_uint(y.x) + (__float_as_uint(t.x) << 23)),
-                       __uint_as_float(__float_as_uint(y.y) + (__float_as_uint(t.y) << 23)));
+    return mul2(y, make_float2(__uint_as_float(__float_as_uint(t.x) << 23), __uint_as_float(__float_as_uint(t.y) << 23)));
 }
 // v[e] of lane i and v[i] of lane e change places among four lanes
 __device__ __forceinline__ void transpose4(uint4 (&v)[4])

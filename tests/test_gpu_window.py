@@ -450,3 +450,32 @@ def test_many_small_weights_beside_one_that_counts_for_nothing(rkv, dtype, d, B,
                 # |q| |k| = d at most, values up to 1 larger: within what attention_tolerance counts on, whose `size` is that of these values
                 over = (s.out[b:b + 1, h * G:(h + 1) * G].double() - ref).abs() - attention_tolerance(ref, size, L, d, s.out.dtype)
                 assert float(over.max()) <= 0, (k, b, h, float((over / size).max()))
+
+
+@pytest.mark.parametrize("dtype,d", SHAPES)
+@pytest.mark.parametrize("window,paged", [(0, False), (30, True)])
+def test_values_that_a_token_does_not_see_count_for_nothing(rkv, dtype, d, window, paged):
+    """Rows that other tokens of the call see, with values as large as the type has them: not a bit of the tokens that do not see them changes."""
+    s = Setup(rkv, dtype, d, 2, 8, [100, 300, 640], [100, 150, 33], 640, window, 0, paged=paged).run()
+    want = s.out.clone()
+    late = torch.zeros(640, dtype=torch.bool, device="cuda")
+    late[[60, 200, 222, 260, 627, 636]] = True
+    rows = late.view(1, 1, 640, 1).expand(3, 2, 640, d)
+    most = torch.full_like(rows, 0x7E if dtype == "fp8" else 1, dtype=torch.uint8)
+    most = most.view(TYPES[dtype]) if dtype == "fp8" else torch.full_like(rows, torch.finfo(TYPES[dtype]).max, dtype=TYPES[dtype])
+    if paged:
+        mine = s.table.clamp_min(0).long()                   # (pages that nobody sees have no entry)
+        for page, spot in zip(mine.flatten(), rows.reshape(-1, 128, d)):
+            s.v[page] = torch.where(spot, most.reshape(-1, 128, d)[0], s.v[page])
+    else:
+        s.v.copy_(torch.where(rows, most, s.v))
+    assert s.call() == 0
+    torch.cuda.synchronize()
+    first, blind = 0, 0
+    for b, (L, n) in enumerate(zip(s.lens, s.new)):
+        sees = (visible(L, n, window, 0) & late[:L]).any(1)
+        for t in torch.nonzero(~sees).flatten().tolist():
+            assert torch.equal(s.out[first + t], want[first + t]), (b, t)
+            blind += 1
+        first += n
+    assert blind >= 60
