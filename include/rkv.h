@@ -366,7 +366,7 @@ RKV_API int rkv_append_rotary(const rkv_desc_t *desc, void *k_cache, void *v_cac
  * Rows of the caches that no new token sees are not read, nor their pages' entries where a whole page of 128 rows is such, and may hold
  * anything; the rows that some new token sees hold finite values (a NaN or infinity there may reach every new token of the sequence).  A sequence
  * whose length is invalid or less than its new tokens gives zero rows and RKV_ERR_INVALID_ARG in desc->device_status; so does a page that does not
- * exist, whose rows count as zeros.
+ * exist, whose rows count as zeros.  A query that holds a NaN gives NaN for its token and head and changes no other.
  * bf16 and 8-bit caches: bf16 products on the tensor cores, fp32 accumulation and softmax; fp32 caches: fp32 throughout.
  * head_dim 64, 128 or 256, any group.  desc->workspace holds rkv_window_workspace_bytes(): partial results of calls whose keys are split between
  * blocks (calls of few rows), and a bf16 copy of the rows that a call of several tokens sees of 8-bit caches; often 0.  Enqueues one to three

@@ -285,8 +285,12 @@ __global__ void __launch_bounds__(kAttThreads, (G <= 4 && sizeof(T) == 2) ? 2 : 
                 const float m_new = fmaxf(m_run[g], m);
                 // (a warp whose rows all lie beyond the length keeps m = -inf: nothing to rescale, weights 0)
                 const float a = m_new == -INFINITY ? 1.f : exp2f(m_run[g] - m_new);
-                const float w0 = m_new == -INFINITY ? 0.f : exp2f(sv[0][g] - m_new);
-                const float w1 = m_new == -INFINITY ? 0.f : exp2f(sv[1][g] - m_new);
+                float w0 = m_new == -INFINITY ? 0.f : exp2f(sv[0][g] - m_new);
+                float w1 = m_new == -INFINITY ? 0.f : exp2f(sv[1][g] - m_new);
+                if constexpr (kMore) {                                   // a query that is no number: neither are its weights
+                    if (sv[0][g] != sv[0][g]) w0 = sv[0][g];
+                    if (sv[1][g] != sv[1][g]) w1 = sv[1][g];
+                }
                 float wsum = j8 == 0 ? w0 + w1 : 0.f;                    // one lane per row counts
                 wsum += __shfl_xor_sync(0xffffffffu, wsum, 8);
                 wsum += __shfl_xor_sync(0xffffffffu, wsum, 16);
@@ -368,12 +372,12 @@ __global__ void __launch_bounds__(kAttThreads, (G <= 4 && sizeof(T) == 2) ? 2 : 
         if constexpr (kMore) {
             const size_t row = (size_t)b * p.hq + (size_t)h * G + g;
             if (!p.partial) {
-                p.out[row * kHeadDim + c] = den > 0.f ? num / den : 0.f;
+                p.out[row * kHeadDim + c] = den != 0.f ? num / den : 0.f;
                 continue;
             }
             float *part = p.partial + (row * p.slots + p.slot + split) * slot_floats(kHeadDim);
             part[c] = num;
-            if (c == 0) part[kHeadDim] = m, part[kHeadDim + 1] = den;
+            if (c == 0) part[kHeadDim] = den != den ? 0.f : m, part[kHeadDim + 1] = den;
         } else if (p.splits == 1) {
             p.out[((size_t)b * p.hq + (size_t)h * G + g) * kHeadDim + c] = den > 0.f ? num / den : 0.f;
         } else {

@@ -389,6 +389,8 @@ attend_tc_kernel(Args p, const __grid_constant__ MapsFor<Args> maps)
         if constexpr (kMore) *to = __float2bfloat16_rn(v);
         else *to = v;
     };
+    // 0 where no row takes part; kMore: NaN for a query that is no number, as the rows' kernels give (rkv_decode_attention: 0)
+    auto quotient = [](float num, float den) -> float { return (kMore ? den != 0.f : den > 0.f) ? num / den : 0.f; };
     bool merges = p.splits > 1;              // the result is merged with those of other blocks, or other kernels
     if constexpr (kMore) merges = merges || p.others > 0 || p.separate;
 
@@ -550,7 +552,7 @@ attend_tc_kernel(Args p, const __grid_constant__ MapsFor<Args> maps)
             if (g < G) {
                 uint8_t hi[8], lo[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) two_codes(f[e] * scale, hi + e, lo + e);
+                for (int e = 0; e < 8; ++e) two_codes(f[e] * scale + f[e] * 0.f, hi + e, lo + e);      // (an infinity has no code: NaN)
                 *reinterpret_cast<uint2 *>(smem + kOffQ + code_off(g, k0)) = make_uint2(hi[0] | hi[1] << 8 | hi[2] << 16 | (uint32_t)hi[3] << 24, hi[4] | hi[5] << 8 | hi[6] << 16 | (uint32_t)hi[7] << 24);
                 *reinterpret_cast<uint2 *>(smem + kOffQ + code_off(8 + g, k0)) = make_uint2(lo[0] | lo[1] << 8 | lo[2] << 16 | (uint32_t)lo[3] << 24, lo[4] | lo[5] << 8 | lo[6] << 16 | (uint32_t)lo[7] << 24);
                 if ((r & 15) == 0) red[g] = __uint_as_float((uint32_t)(127 - up) << 23) * c2;
@@ -710,7 +712,7 @@ attend_tc_kernel(Args p, const __grid_constant__ MapsFor<Args> maps)
             num[g] *= kScale, den *= kScale;
             if (r >= kDim) continue;                          // (64 dimensions: the padded half of the output)
             if (!merges) {
-                put(out + (size_t)g * kDim + r, den > 0.f ? num[g] / den : 0.f);
+                put(out + (size_t)g * kDim + r, quotient(num[g], den));
             } else {
                 part[g * part_stride + r] = num[g];
                 if (r == 0) {
@@ -780,7 +782,7 @@ attend_tc_kernel(Args p, const __grid_constant__ MapsFor<Args> maps)
                     }
                 }
             }
-            put(out + x, den > 0.f ? num / den : 0.f);
+            put(out + x, quotient(num, den));
         }
         cluster_sync();                     // nobody leaves while its partial result is still being read
     } else if constexpr (kMore) {

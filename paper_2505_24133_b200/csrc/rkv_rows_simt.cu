@@ -214,7 +214,7 @@ __global__ void __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) rows_simt_kerne
             float *dst = p.part + (((size_t)t * p.hq + qh) * p.slots + p.slot + split) * slot_floats(kDim);
 #pragma unroll
             for (int c = 0; c < kDim / 16; ++c) dst[(c >> 2) * 64 + tx * 4 + (c & 3)] = o[i][c];
-            if (tx == 0) dst[kDim] = m[i], dst[kDim + 1] = l[i];
+            if (tx == 0) dst[kDim] = l[i] != l[i] ? 0.f : m[i], dst[kDim + 1] = l[i];      // (no number: the merge must take it in)
         } else {
             TQ *dst = static_cast<TQ *>(p.out) + t * p.out_stride + (size_t)qh * kDim;
 #pragma unroll

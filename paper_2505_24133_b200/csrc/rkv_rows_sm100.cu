@@ -633,7 +633,9 @@ rows_tc_kernel(RowsParams p, int tokens_per_tile, int pieces, int items, const _
                     if (to) *reinterpret_cast<uint4 *>(reinterpret_cast<__nv_bfloat16 *>(to) + c0 + c + (lane & 3) * 8) = v[e];
                 }
             }
-            if (mine && part && half == 0) *reinterpret_cast<float2 *>(part + kDim) = make_float2(ok && T > 0 ? m * c2 : -INFINITY, ok ? l : 0.f);
+            // (a query that is no number leaves no maximum: any finite one makes the merge take the share in)
+            if (mine && part && half == 0)
+                *reinterpret_cast<float2 *>(part + kDim) = make_float2(!ok || T == 0 ? -INFINITY : l != l ? 0.f : m * c2, ok ? l : 0.f);
         }
     }
 

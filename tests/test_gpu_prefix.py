@@ -287,3 +287,21 @@ def test_prefixes_in_front_of_long_caches_of_many_heads(rkv, dtype, d):
             ref, size = attention(q[b:b + 1, heads], keys, values, torch.ones(1, P + L, dtype=torch.bool, device="cuda"))
             over = (out[b:b + 1, heads].double() - ref).abs() - attention_tolerance(ref, size, P + L, d, q.dtype)
             assert float(over.max()) <= 0, (b, h)
+
+
+@pytest.mark.parametrize("dtype,d", SHAPES)
+@pytest.mark.parametrize("batch,prefixes,rows,cap", [(2, 2, 300, 200), (4, 1, 300, 700), (48, 1, 2000, 300), (200, 1, 4000, 130)])
+def test_a_query_that_is_no_number_gives_none(rkv, dtype, d, batch, prefixes, rows, cap):
+    """NaN for that sequence and head whether its prefix is read beside its own rows or apart, and nothing else changes."""
+    s = Setup(rkv, dtype, d, 2, 8, [(37 * b) % cap for b in range(batch)], [rows] * prefixes, cap, rows).run()
+    want = s.out.clone()
+    hit = [(0, 1), (batch - 1, 7)]
+    for b, h in hit:
+        s.q[b, h, 5 + b % 50] = float("nan")
+    assert s.call() == 0
+    torch.cuda.synchronize()
+    assert int(s.status.item()) == 0
+    for b, h in hit:
+        assert s.out[b, h].isnan().all(), (b, h)
+        s.out[b, h] = want[b, h]
+    assert torch.equal(s.out, want)

@@ -479,3 +479,26 @@ def test_values_that_a_token_does_not_see_count_for_nothing(rkv, dtype, d, windo
             blind += 1
         first += n
     assert blind >= 60
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("dtype,d", SHAPES)
+@pytest.mark.parametrize("hkv,G,lens,new,cap,window", [
+    (2, 4, [300, 64, 640], [1, 1, 1], 640, 0), (8, 4, [200 + b for b in range(40)], [1] * 40, 300, 100),      # single tokens, split and not
+    (1, 2, [5000, 4999], [1, 1], 5120, 0), (1, 2, [5000, 4999], [2, 3], 5120, 0),                             # few rows over many keys
+    (2, 4, [300, 400], [100, 37], 640, 150), (8, 4, [700, 600, 650], [500, 600, 333], 720, 0)])               # prompts
+def test_a_query_that_is_no_number_gives_none(rkv, value, dtype, d, hkv, G, lens, new, cap, window):
+    """NaN for that token and head however the call is cut into blocks, and nothing else changes.  (An infinity: every score is infinite, of either
+    sign, or NaN.)"""
+    s = Setup(rkv, dtype, d, hkv, hkv * G, lens, new, cap, window, 0, offsets=max(new) > 1).run()
+    want, total = s.out.clone(), sum(new)
+    hit = [(0, 1), (total - 1, hkv * G - 1), (total // 2, 0)]
+    for t, h in hit:
+        s.q[t, h, (7 * t + 3) % d] = value
+    assert s.call() == 0
+    torch.cuda.synchronize()
+    assert int(s.status.item()) == 0
+    for t, h in hit:
+        assert s.out[t, h].isnan().all(), (t, h)
+        s.out[t, h] = want[t, h]
+    assert torch.equal(s.out, want)
