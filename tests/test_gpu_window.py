@@ -390,7 +390,8 @@ def test_maxima_that_move_between_the_halves_of_a_tile(rkv, dtype, d, G, new):
 
 
 def shared_pages(dtype, d, heads, cap, gen, pages=500):
-    """Pools of pages that all heads' tables draw from, so that long caches of many heads take little room: pool of K, of V, table [heads, cap / 128]."""
+    """Pools of pages that all heads' tables draw from (the attention only reads them), so that long caches of many heads take little room: pool of K,
+    of V, table [heads, cap / 128]."""
     pools = [torch.randn(pages, 128, d, generator=gen, device="cuda").to(TYPES[dtype]) for _ in range(2)]
     table = torch.stack([torch.randperm(pages, generator=gen, device="cuda")[:cap // 128] for _ in range(heads)])
     return pools[0], pools[1], table.to(torch.int32)
@@ -502,3 +503,31 @@ def test_a_query_that_is_no_number_gives_none(rkv, value, dtype, d, hkv, G, lens
         assert s.out[t, h].isnan().all(), (t, h)
         s.out[t, h] = want[t, h]
     assert torch.equal(s.out, want)
+
+
+@pytest.mark.parametrize("dtype,d", SHAPES)
+@pytest.mark.parametrize("lens,new,window", [([700, 640], [200, 1], 0), ([700, 640], [350, 100], 300), ([700, 1, 640], [1, 1, 1], 0), ([700] * 40, [1] * 40, 0)])
+@pytest.mark.parametrize("way", ["up", "down", "peak", "valley"])
+def test_large_scores_in_every_form(rkv, dtype, d, lens, new, window, way):
+    """Scores between -370 and 370 that grow, fall, or turn inside the cache: maxima that move at every tile or never again, exponentials from far below
+    the smallest number to the reference of the weights and beyond it; prompts, pieces of prompts and single tokens."""
+    s = Setup(rkv, dtype, d, 1, 4, lens, new, 700, window, 0, offsets=max(new) > 1)
+    x = torch.linspace(-8, 8, 700, device="cuda")
+    ramp = {"up": x, "down": -x, "peak": 8 - 2 * x.abs(), "valley": 2 * x.abs() - 8}[way] * (128 / d) ** 0.5
+    for k in (s.k, s.k0):
+        k.copy_(ramp[:, None].expand(700, d).to(k.dtype).expand_as(k))
+    s.q.copy_((s.q.float() * 0.25 + 4.0).to(s.q.dtype))
+    assert s.call() == 0
+    torch.cuda.synchronize()
+    assert int(s.status.item()) == 0
+    first = 0
+    for b, (L, n) in enumerate(zip(s.lens, s.new)):
+        ref, size = attention(s.q[first:first + n], s.k0[b, 0, :L], s.v0[b, 0, :L], visible(L, n, window, 0))
+        # products of 8-bit or bf16 factors are exact; scores up to 8 * (4 + 4 * 0.25 / d ** 0.5) * 128 ** 0.5 < 400, their sums off by (d + 2) 2^-24
+        # of that, of 32-bit factors by as much again; then the factor log2(e) / sqrt(d) and the difference from the maximum, each a rounding of at
+        # most 600 in base 2: 4 * 600 * 2^-24 in all.  Twice that for numerator and denominator, 2^-12 for the exponentials, bf16 weights, the output.
+        off = 2 * (d + 2) * 2.0 ** -24 * 400 + 4 * 600 * 2.0 ** -24
+        tol = (ref.abs() + size) * 2.0 ** -8 * (0 if dtype == "f32" else 1) + size * 2 * (off + 2.0 ** -12)
+        got = s.out[first:first + n].double()
+        assert torch.isfinite(got).all() and ((got - ref).abs() <= tol).all(), (b, float(((got - ref).abs() - tol).max()))
+        first += n
