@@ -305,3 +305,76 @@ def test_a_query_that_is_no_number_gives_none(rkv, dtype, d, batch, prefixes, ro
         assert s.out[b, h].isnan().all(), (b, h)
         s.out[b, h] = want[b, h]
     assert torch.equal(s.out, want)
+
+
+def _mixed_chain(rkv, dtype, d, B, wait):
+    """Pieces of prompts and steps of samples in turn, all calls on one workspace; with `wait`, each call finished before the next."""
+    from tokens_util import rotation_table
+    hkv, hq, cap, rows = 4, 16, 768, 2048
+    gen = torch.Generator(device="cuda").manual_seed(52)
+    draw = lambda t, *shape: torch.randn(*shape, generator=gen, device="cuda").to(t[dtype])  # noqa: E731
+    k, v, pk, pv = draw(TYPES, B, hkv, cap, d), draw(TYPES, B, hkv, cap, d), draw(TYPES, 2, hkv, rows, d), draw(TYPES, 2, hkv, rows, d)
+    seq = torch.tensor([(5 * b) % 200 for b in range(B)], dtype=torch.int32, device="cuda")
+    plens = torch.tensor([rows, 1777], dtype=torch.int32, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    desc = descriptor(rkv, B, hkv, hq, d, dtype, status)
+    prefix, rotary, one = rkv.rkv_prefix(pk, pv, plens), rkv.rkv_rotary(rotation_table(1024, 32), 32), rkv.rkv_tokens(B, 1)
+    pieces = []
+    for i in range(4):
+        ends = torch.tensor([(7 * b + i) % 40 for b in range(B)]).cumsum(0).tolist()
+        pieces.append(rkv.rkv_tokens(ends[-1], 40, torch.tensor([0] + ends, dtype=torch.int32, device="cuda")))
+    need = max([256, rkv.rkv_prefix_workspace_bytes(desc, cap - 1, 1, prefix)] +
+               [rkv.rkv_window_workspace_bytes(desc, cap - 1, 1, t, w, 4) for t in pieces + [one] for w in (0, 100)])
+    room = torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda")
+    desc.workspace, desc.workspace_bytes = room.data_ptr(), need
+
+    def calls(t, window, samples):
+        n = t.total
+        kn, vn, qn = draw(WIDE, n, hkv, d), draw(WIDE, n, hkv, d), draw(WIDE, n, hq, d)
+        q, a, w = (torch.zeros_like(qn) for _ in range(3))
+        outs.extend([a, w])
+        yield lambda: rkv.rkv_append_rotary(desc, k, v, kn, vn, seq, cap - 1, 1, t, rotary, qn, q)
+        if samples:
+            yield lambda: rkv.rkv_prefix_attention(desc, k, v, q, seq, a, cap - 1, 1, prefix)
+        yield lambda: rkv.rkv_window_attention(desc, k, v, q, seq, w, cap - 1, 1, t, window, 4)
+
+    outs, todo = [], []
+    for i, t in enumerate(pieces):
+        todo += calls(t, 100 * (i & 1), False)
+        for _ in range(3):
+            todo += calls(one, 0, True)
+    torch.cuda.synchronize()
+    for call in todo:
+        assert call() == 0
+        if wait:
+            torch.cuda.synchronize()
+    torch.cuda.synchronize()
+    assert int(status.item()) == 0
+    return outs + [k, v, seq]
+
+
+@pytest.mark.parametrize("dtype,d", SHAPES)
+@pytest.mark.parametrize("batch", [2, 24])
+def test_pieces_of_prompts_and_steps_of_every_type_without_waiting(rkv, dtype, d, batch):
+    """Every chain of kernels behind every other one on the same workspace; prefixes read beside the own rows, and apart."""
+    want = _mixed_chain(rkv, dtype, d, batch, True)
+    for _ in range(3):
+        for a, b in zip(_mixed_chain(rkv, dtype, d, batch, False), want):
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+@pytest.mark.parametrize("dtype,d", SHAPES)
+@pytest.mark.parametrize("batch,prefixes,rows,cap", [(2, 2, 384, 256), (48, 1, 2048, 384), (200, 1, 4096, 128)])
+@pytest.mark.parametrize("paged", [False, True])
+def test_captured_calls_of_every_type(rkv, dtype, d, batch, prefixes, rows, cap, paged):
+    s = Setup(rkv, dtype, d, 2, 8, [(37 * b) % cap for b in range(batch)], [rows - 5] * prefixes, cap, rows, paged=paged).run()
+    want = s.out.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        for _ in range(3):
+            assert s.call() == 0
+    for _ in range(3):
+        s.out.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(s.out, want)

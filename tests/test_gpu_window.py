@@ -531,3 +531,36 @@ def test_large_scores_in_every_form(rkv, dtype, d, lens, new, window, way):
         got = s.out[first:first + n].double()
         assert torch.isfinite(got).all() and ((got - ref).abs() <= tol).all(), (b, float(((got - ref).abs() - tol).max()))
         first += n
+
+
+@pytest.mark.parametrize("dtype,d", SHAPES)
+@pytest.mark.parametrize("new", [[1, 1, 1], [100, 64, 37]])
+def test_windows_and_sinks_up_to_the_largest_number(rkv, dtype, d, new):
+    """They see all rows up to the token's own, as window 0 does."""
+    most = 2 ** 31 - 1
+    for window, sinks in ((most, 0), (most, most), (1, most), (most - 1, 5), (650, most)):
+        s = Setup(rkv, dtype, d, 2, 8, [300, 100, 640], new, 640, 0, 0, offsets=max(new) > 1)
+        s.window, s.sinks = window, sinks
+        s.workspace(s.desc)
+        assert s.call() == 0
+        torch.cuda.synchronize()
+        s.window, s.sinks = 0, 0
+        s.check()
+
+
+@pytest.mark.parametrize("dtype,d", SHAPES)
+@pytest.mark.parametrize("lens,new", [([300, 64, 640], [1, 1, 1]), ([300, 64, 640], [100, 64, 37]), ([5000, 4999], [3, 2])])
+@pytest.mark.parametrize("paged", [False, True])
+def test_captured_calls_of_every_type(rkv, dtype, d, lens, new, paged):
+    """Three calls in one graph, whose kernels start early beside one another and share the workspace."""
+    s = Setup(rkv, dtype, d, 2, 8, lens, new, 5120 if max(lens) > 640 else 640, 0, 0, offsets=max(new) > 1, paged=paged).run()
+    want = s.out.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        for _ in range(3):
+            assert s.call() == 0
+    for _ in range(3):
+        s.out.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(s.out, want)
