@@ -348,7 +348,8 @@ typedef struct rkv_rotary {
  *   q_new, q_out  [total][n_q_heads][head_dim] of the queries' type, both or neither NULL; q_out may be q_new (with out_stride = q_stride)
  * Products in fp32, rounded once; what is not rotated and keeps its type is copied bit for bit.  All tensors 16-byte aligned.
  * A sequence that the tokens do not fit into (or whose length is invalid), or whose positions leave the table, is left as it is, its rows of q_out
- * too, and RKV_ERR_INVALID_ARG is written to desc->device_status.
+ * too, and RKV_ERR_INVALID_ARG is written to desc->device_status.  Rows of a page that does not exist are recorded so too and dropped; the others enter
+ * and the length grows.
  * One launch for one token or a few per sequence, else two; no workspace.
  */
 RKV_API int rkv_append_rotary(const rkv_desc_t *desc, void *k_cache, void *v_cache, const void *k_new, const void *v_new,
@@ -367,10 +368,16 @@ RKV_API int rkv_append_rotary(const rkv_desc_t *desc, void *k_cache, void *v_cac
  * anything; the rows that some new token sees hold finite values (a NaN or infinity there may reach every new token of the sequence).  A sequence
  * whose length is invalid or less than its new tokens gives zero rows and RKV_ERR_INVALID_ARG in desc->device_status; so does a page that does not
  * exist, whose rows count as zeros.  A query that holds a NaN gives NaN for its token and head and changes no other.
- * bf16 and 8-bit caches: bf16 products on the tensor cores, fp32 accumulation and softmax; fp32 caches: fp32 throughout.
- * head_dim 64, 128 or 256, any group.  desc->workspace holds rkv_window_workspace_bytes(): partial results of calls whose keys are split between
- * blocks (calls of few rows), and a bf16 copy of the rows that a call of several tokens sees of 8-bit caches; often 0.  Enqueues one to three
- * kernels on `stream`.
+ * head_dim 64, 128 or 256, any group; sums, softmax and accumulation in fp32.  What takes part in the products:
+ *   bf16 and 8-bit caches of 64 or 128 dimensions, groups up to 128: tensor cores, weights rounded to bf16
+ *   single tokens (tokens->offsets NULL, longest 1, tokens back to back) of groups up to 8, over capacities, or windows with their sinks, of up to
+ *   448 tiles of 128 rows: bf16 caches of 64 or 128 dimensions with weights of two bf16 parts; 8-bit caches of 128 dimensions as they are
+ *   stored, weights rounded to fp16 (2^-40 at the smallest), query elements to 2^-21 of their head's largest where that is more than their own bits
+ *   everything else: fp32 products of the values as they are, without tensor cores
+ * desc->workspace holds rkv_window_workspace_bytes(): partial results of calls whose keys are split between blocks of their own (calls of few rows),
+ * and, for 8-bit caches of 64 or 128 dimensions, a bf16 copy of the rows that the call sees, unless it is one of the single tokens above (also where
+ * few tokens see long caches: the copy then moves five times the cache's bytes); often 0.  Enqueues one to three kernels on `stream`.  After
+ * RKV_ERR_TIMEOUT in desc->device_status the output is not to be used.
  */
 RKV_API size_t rkv_window_workspace_bytes(const rkv_desc_t *desc, int32_t budget, int32_t buffer, const rkv_tokens_t *tokens,
                                           int32_t window, int32_t sinks);
@@ -391,13 +398,14 @@ typedef struct rkv_prefix {
 
 /*
  * rkv_decode_attention for a batch that shares long prefixes: every sequence's query attends over its prefix's rows and its own cache, in one
- * softmax; a prefix's keys and values are read once for all of its sequences.
+ * softmax; a prefix's keys and values are read once for all of its sequences (short prefixes, or those of one sequence, by every sequence again).
  *   q_new, out  [batch][n_q_heads][head_dim] as in rkv_window_attention (out has q_new's type)
  *   seq_lens    [batch], own rows of each sequence, 0 allowed; a value outside [0, budget + buffer], like a prefix length outside [0, rows], counts as 0
  *               and is recorded as RKV_ERR_INVALID_ARG
  * The sequences' own caches may be compressed, appended to and paged as ever; the prefix is not compressed with them.
  * head_dim, groups, types and arithmetic as rkv_window_attention; rows beyond the lengths are not read.  desc->workspace holds
- * rkv_prefix_workspace_bytes() (partial results; a bf16 copy of 8-bit prefixes).  Enqueues up to four kernels on `stream`.
+ * rkv_prefix_workspace_bytes(): partial results, a bf16 copy of 8-bit prefixes, and of the sequences' own 8-bit rows where rkv_window_attention
+ * would make one for single tokens.  Enqueues up to five kernels on `stream`.  After RKV_ERR_TIMEOUT in desc->device_status the output is not to be used.
  */
 RKV_API size_t rkv_prefix_workspace_bytes(const rkv_desc_t *desc, int32_t budget, int32_t buffer, const rkv_prefix_t *prefix);
 RKV_API int rkv_prefix_attention(const rkv_desc_t *desc, const void *k_cache, const void *v_cache, const void *q_new,

@@ -10,7 +10,7 @@ int source_of(int dtype, int d) { return dtype == RKV_FP8_E4M3 ? 1 : d == 64 ? 2
 
 }  // namespace
 
-// `tiles`: key tiles that a token sees at most.
+// `tiles`: key tiles that a token sees at most: 448, what blocks of two chunks in a cluster take (the rows' kernel takes longer ones).
 bool attend_more_supported(int dtype, int d, int group, long long tiles)
 {
     return attend_supported(group, dtype, d) && tiles <= (dtype == RKV_F32 ? 1ll << 23 : (long long)kTcMaxSplits * 2 * kTcChunkTiles);
